@@ -74,7 +74,11 @@ typedef enum {
   AMS_ENOMEM = -6     /* a workspace is smaller than required */
 } ams_status;
 
-typedef enum { AMS_F32 = 0, AMS_BF16 = 1 } ams_dtype;
+typedef enum {
+  AMS_F32 = 0,
+  AMS_BF16 = 1,
+  AMS_F16 = 2 /* tensors of the ams_qcache_ calls only: no model or context takes it */
+} ams_dtype;
 
 /* Decoder dimensions.  d_model = n_heads * head_dim; head_dim even and at
  * most 128; d_model a multiple of 128; d_ffn a multiple of 128;
@@ -179,6 +183,96 @@ ams_status ams_index_hash(const void* data, size_t n_bytes, int32_t seg_bytes, v
  * ordered.  Other arguments and errors as ams_index_hash. */
 ams_status ams_index_hash_noalloc(const void* data, size_t n_bytes, int32_t seg_bytes, uint64_t* out_hash,
                                   void* stream);
+
+/* ---- 8-bit K/V cache --------------------------------------------------- */
+
+/* One layer's keys and values in 8 bits, with a power-of-two scale for every
+ * block of 64 positions (a page) and head: half the bytes of an fp16 cache, so
+ * twice the contexts fit the GPU (paper section 3.2.2, Layered Storage of
+ * Action Context) and a decode step, which streams the cache, reads half.
+ * All arrays are on the current device, 16-byte aligned, owned by the caller:
+ *   k        [n_pages][n_kv_heads][64][head_dim]     e4m3 codes
+ *   v        [n_pages][n_kv_heads][16][head_dim][4]  e4m3 codes, position t of a
+ *            page at [t / 4][:][t % 4]
+ *   k_scale, v_scale  fp32 [n_pages][n_kv_heads], powers of two: a code stands for
+ *            its value times its page's scale
+ *   k_bounds int8 [n_pages][n_kv_heads][2][head_dim]: per channel the largest
+ *            ceil(key / 4), then the smallest floor(key / 4) over the page's
+ *            positions, in units of the scale (what a selection of pages reads)
+ *   page_table  int32 [rows][pages_per_row]: the page of each row's 64-position
+ *            block; entries outside [0, n_pages) hold no positions (an append
+ *            skips them, an attention does not see them).
+ * e4m3: 1 sign, 4 exponent (bias 7) and 3 mantissa bits, no infinities, largest
+ * value 448.  n_kv_heads in [1, 1024], head_dim 64 or 128, n_pages in [1, 2^28],
+ * rows in [1, 65535], pages_per_row in [1, 16384].
+ * The arrays need no initial values: a page's first position sets its scales and bounds. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int8_t* k_bounds;
+  const int32_t* page_table;
+  int32_t n_pages, n_kv_heads, head_dim, rows, pages_per_row;
+} ams_qcache;
+
+/* The new tokens of a call are packed row after row: row b's are tokens
+ * tok_off[b] .. tok_off[b + 1] - 1 (device int32 [rows + 1], increasing from 0
+ * to n_tok; a row may have none) and end at position kv_len[b] - 1 (device int32
+ * [rows], the row's length with them, at most 64 * pages_per_row).  max_new >= 1
+ * is at least the longest row's number of new tokens: it sizes the launch, and
+ * what a row has beyond it is undefined.  Nothing is read back, so the calls can be
+ * captured into a HIP graph and replayed with other lengths in the same arrays.
+ *
+ * Writes the new tokens' keys and values into the rows' pages.  k, v: device
+ * [n_tok][n_kv_heads][head_dim] of type dtype (AMS_F32, AMS_BF16 or AMS_F16),
+ * token strides ldk and ldv elements (>= n_kv_heads * head_dim), any alignment of
+ * the type.  Each page and head takes the least scale 2^e, e >= -32, with
+ * |x| <= 448 * 2^e for its new values; a page that already holds earlier
+ * positions of the row keeps its scale when that is larger, and otherwise its
+ * codes are rounded again to the new scale (exact but for e4m3 subnormals).
+ * Values saturate at +-65504.  A token whose key or value of a head holds a NaN
+ * gets a NaN key there (every query of that head that sees the token reads NaN;
+ * none that does not) and zeros for its NaN values.  Tokens at negative
+ * positions are not stored.  A page that a call writes belongs to one row of it.
+ * Errors: AMS_EINVAL, AMS_ENODEV, AMS_EHIP. */
+ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, const int32_t* kv_len, int32_t n_tok,
+                             int32_t max_new, const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t dtype,
+                             void* stream);
+
+/* Bytes of device workspace ams_qcache_attend needs for these sizes (at least 1;
+ * 0 if an argument is invalid).  Only the dimensions of `cache` are read. */
+size_t ams_qcache_workspace_bytes(const ams_qcache* cache, int32_t n_heads, int32_t n_tok, int32_t max_new,
+                                  int32_t max_len, int32_t n_select);
+
+/* Causal attention of the new tokens over what their rows hold, themselves
+ * included (call it after the append): token i of row b's n sees the positions
+ * below kv_len[b] - n + 1 + i; a token that sees none gets zeros.
+ *   q, out: device [n_tok][n_heads][head_dim] of type dtype, token strides ldq and
+ *           ldo elements, any alignment of the type; n_heads a multiple of
+ *           n_kv_heads (query head j reads KV head j / (n_heads / n_kv_heads)).
+ *           Tokens that no row owns keep their out.  out and q may not overlap.
+ *   scale:  softmax(scale * q . k), finite and > 0;
+ *   max_len >= 1: about the longest kv_len.  It chooses how the work is split and
+ *           bounds nothing.
+ *   n_select: 0 attends to everything.  Above 0 (at most 16384), each token and KV
+ *           head attends to n_select pages of its row: the one that holds its
+ *           last visible position and those whose bounds promise the largest
+ *           scores, ties to the lower page -- to all when n_select or fewer are
+ *           visible.  The score: with x such that the largest |q| of the group's
+ *           heads is in [2^(x-1), 2^x), q^ = rint(q 2^(7-x)) clamped to +-127 and the
+ *           page's bounds hi, lo and key scale s,
+ *             s * max over the group's heads of sum_d max(q^_d, 0) hi_d + min(q^_d, 0) lo_d,
+ *           sums of whole numbers, so the choice does not depend on their order.
+ *   selected: NULL, or device int32 [n_tok][n_kv_heads][n_select] receiving the
+ *           chosen pages of the row in increasing order, then -1 (n_select > 0).
+ *   ws:     device memory of ams_qcache_workspace_bytes, 16-byte aligned; used
+ *           until the call has completed on its stream.
+ * fp16 and bf16: queries and probabilities enter the products as fp16, queries
+ * scaled by a power of two first; fp32: as fp16 pairs (about 22 bits).  Statistics
+ * and sums are fp32.  Errors: AMS_EINVAL, AMS_ENOMEM, AMS_ENODEV, AMS_EHIP. */
+ams_status ams_qcache_attend(const ams_qcache* cache, const int32_t* tok_off, const int32_t* kv_len, int32_t n_tok,
+                             int32_t max_new, int32_t max_len, int32_t n_heads, const void* q, int64_t ldq, void* out,
+                             int64_t ldo, int32_t dtype, float scale, int32_t n_select, int32_t* selected, void* ws,
+                             size_t ws_bytes, void* stream);
 
 /* ---- context ---------------------------------------------------------- */
 

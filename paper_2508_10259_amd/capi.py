@@ -11,7 +11,7 @@ import os
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libams.so")
 
 AMS_OK, AMS_EINVAL, AMS_ESTATE, AMS_ECAPACITY, AMS_ENODEV, AMS_EHIP, AMS_ENOMEM = 0, -1, -2, -3, -4, -5, -6
-AMS_F32, AMS_BF16 = 0, 1
+AMS_F32, AMS_BF16, AMS_F16 = 0, 1, 2
 AMS_CTX_SHARE_PREFIX = 1
 STATE_EMPTY, STATE_READY, STATE_INVALID, STATE_OFFLOADED = 0, 1, 2, 3
 
@@ -33,6 +33,13 @@ class FlowHead(C.Structure):
                 ("n_tokens", C.c_int32)]
 
 
+class QCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("k_bounds", C.c_void_p), ("page_table", C.c_void_p), ("n_pages", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("rows", C.c_int32),
+                ("pages_per_row", C.c_int32)]
+
+
 # name -> (restype, argtypes)
 SIGNATURES = {
     "ams_status_str": (C.c_char_p, [C.c_int32]),
@@ -47,6 +54,13 @@ SIGNATURES = {
     "ams_index_hash": (C.c_int32, [C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p,
                                    C.c_void_p]),
     "ams_index_hash_noalloc": (C.c_int32, [C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p, C.c_void_p]),
+    "ams_qcache_append": (C.c_int32, [C.POINTER(QCache), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p,
+                                      C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p]),
+    "ams_qcache_workspace_bytes": (C.c_size_t, [C.POINTER(QCache), C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                                C.c_int32]),
+    "ams_qcache_attend": (C.c_int32, [C.POINTER(QCache), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                                      C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_float,
+                                      C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "ams_ctx_workspace_bytes": (C.c_size_t, [C.POINTER(ModelCfg), C.c_int32, C.c_int32, C.c_int32]),
     "ams_ctx_create": (C.c_int32, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t,
                                    C.POINTER(C.c_void_p)]),

@@ -6,7 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
-
+#include <cmath>
 #include <string>
 #include <vector>
 
@@ -83,6 +83,10 @@ bool dev_range(const void* p, size_t bytes, int dev, const char* what, std::stri
   }
   return true;
 }
+
+// Workgroups of one launch of the 8-bit cache's kernels (of 1,024 threads at most: a grid has fewer than
+// 2^32 threads).
+constexpr int64_t QCACHE_MAX_BLOCKS = (int64_t)1 << 22;
 
 bool aligned256(const void* p) { return ((uintptr_t)p & 255) == 0; }
 
@@ -459,6 +463,164 @@ ams_status ams_index_hash_noalloc(const void* data, size_t n_bytes, int32_t seg_
   r = ams::hash_segments(data, n_bytes, seg_bytes, scratch, st);
   if (r == hipSuccess) r = ams::hash_merge(scratch, k, n_bytes, out_hash, st);
   if (r != hipSuccess) return fail(AMS_EHIP, std::string("index hash: ") + hipGetErrorString(r));
+  return AMS_OK;
+}
+
+namespace {
+
+// What the three 8-bit cache calls share: the dimensions, then the device arrays.
+bool qcache_dims(const ams_qcache* c, std::string& e) {
+  if (!c) e = "cache is NULL";
+  else if (c->head_dim != 64 && c->head_dim != 128) e = "head_dim must be 64 or 128";
+  else if (c->n_kv_heads < 1 || c->n_kv_heads > 1024) e = "n_kv_heads must be in [1, 1024]";
+  else if (c->n_pages < 1 || c->n_pages > (1 << 28)) e = "n_pages must be in [1, 2^28]";
+  else if (c->rows < 1 || c->rows > 65535) e = "rows must be in [1, 65535]";
+  else if (c->pages_per_row < 1 || c->pages_per_row > 16384) e = "pages_per_row must be in [1, 16384]";
+  else return true;
+  return false;
+}
+
+bool qcache_sizes(const ams_qcache* c, int32_t n_heads, int32_t n_tok, int32_t max_new, int32_t max_len,
+                  int32_t n_select, std::string& e) {
+  if (!qcache_dims(c, e)) return false;
+  if (n_heads < 1 || n_heads > 65536 || n_heads % c->n_kv_heads) e = "n_heads must be a multiple of n_kv_heads, at most 65536";
+  else if (n_tok < 0) e = "n_tok must be >= 0";
+  else if (max_new < 1) e = "max_new must be >= 1";
+  else if (max_len < 1) e = "max_len must be >= 1";
+  else if (n_select < 0 || n_select > 16384) e = "n_select must be in [0, 16384]";
+  else return true;
+  return false;
+}
+
+bool qcache_type(int32_t dtype, std::string& e) {
+  if (dtype == AMS_F32 || dtype == AMS_BF16 || dtype == AMS_F16) return true;
+  e = "dtype must be AMS_F32, AMS_BF16 or AMS_F16";
+  return false;
+}
+
+// A [n_tok][heads][head_dim] tensor with a token stride of ld elements.
+bool qcache_tensor(const void* p, int64_t ld, int32_t n_tok, int64_t width, int32_t dtype, int dev, const char* what,
+                   std::string& e) {
+  const int64_t es = dtype == AMS_F32 ? 4 : 2;
+  if (ld < width || ld > ((int64_t)1 << 40)) {
+    e = std::string(what) + ": token stride must be at least heads * head_dim (and at most 2^40) elements";
+    return false;
+  }
+  if ((uintptr_t)p % es) {
+    e = std::string(what) + " is not aligned to its type";
+    return false;
+  }
+  return dev_range(p, (size_t)(((int64_t)(n_tok - 1) * ld + width) * es), dev, what, e);
+}
+
+bool qcache_arrays(const ams_qcache* c, const int32_t* tok_off, const int32_t* kv_len, int dev, std::string& e) {
+  const void* p[] = {c->k, c->v, c->k_scale, c->v_scale, c->k_bounds};
+  for (const void* x : p)
+    if ((uintptr_t)x & 15) {
+      e = "the cache's arrays must be 16-byte aligned";
+      return false;
+    }
+  if (((uintptr_t)c->page_table | (uintptr_t)tok_off | (uintptr_t)kv_len) & 3) {
+    e = "page_table, tok_off and kv_len must be 4-byte aligned";
+    return false;
+  }
+  const size_t ph = (size_t)c->n_pages * c->n_kv_heads, d = c->head_dim;
+  return dev_range(c->k, ph * 64 * d, dev, "cache k", e) && dev_range(c->v, ph * 64 * d, dev, "cache v", e) &&
+         dev_range(c->k_scale, ph * 4, dev, "cache k_scale", e) && dev_range(c->v_scale, ph * 4, dev, "cache v_scale", e) &&
+         dev_range(c->k_bounds, ph * 2 * d, dev, "cache k_bounds", e) &&
+         dev_range(c->page_table, (size_t)c->rows * c->pages_per_row * 4, dev, "cache page_table", e) &&
+         dev_range(tok_off, ((size_t)c->rows + 1) * 4, dev, "tok_off", e) &&
+         dev_range(kv_len, (size_t)c->rows * 4, dev, "kv_len", e);
+}
+
+ams::QCache qcache_view(const ams_qcache* c) {
+  return ams::QCache{(uint8_t*)c->k, (uint8_t*)c->v, c->k_scale, c->v_scale, c->k_bounds, c->page_table,
+                     c->n_pages, c->n_kv_heads, c->head_dim, c->rows, c->pages_per_row};
+}
+
+ams::QAttendPlan qcache_plan(const ams_qcache* c, int32_t n_heads, int32_t n_tok, int32_t max_new, int32_t max_len,
+                             int32_t n_select) {
+  return ams::qcache_attend_plan(c->rows, n_heads, c->n_kv_heads, c->head_dim, n_tok, std::min(max_new, n_tok),
+                                 std::min(max_len, c->pages_per_row * 64), std::min(n_select, c->pages_per_row));
+}
+size_t align16(size_t x) { return (x + 15) & ~(size_t)15; }
+
+}  // namespace
+
+ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, const int32_t* kv_len, int32_t n_tok,
+                             int32_t max_new, const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t dtype,
+                             void* stream) {
+  g_err.clear();
+  std::string e;
+  if (!qcache_sizes(cache, cache ? cache->n_kv_heads : 0, n_tok, max_new, 1, 0, e) || !qcache_type(dtype, e))
+    return fail(AMS_EINVAL, e);
+  if (n_tok == 0) return AMS_OK;
+  max_new = std::min(max_new, n_tok);
+  if (((int64_t)(max_new + 62) / 64 + 1) * cache->n_kv_heads * cache->rows > QCACHE_MAX_BLOCKS)
+    return fail(AMS_EINVAL, "too many pages for one call: rows * n_kv_heads * max_new / 64 is above 2^22");
+  int dev = 0;
+  if (int s = current_device(&dev, e)) return fail(s, e);
+  const int64_t width = (int64_t)cache->n_kv_heads * cache->head_dim;
+  if (!qcache_arrays(cache, tok_off, kv_len, dev, e) || !qcache_tensor(k, ldk, n_tok, width, dtype, dev, "k", e) ||
+      !qcache_tensor(v, ldv, n_tok, width, dtype, dev, "v", e))
+    return fail(AMS_EINVAL, e);
+  const ams::QSegs sg{nullptr, tok_off, nullptr, kv_len, 0, cache->rows, n_tok, max_new};
+  hipError_t r = ams::qcache_append(qcache_view(cache), sg, k, ldk, v, ldv, dtype, nullptr, (hipStream_t)stream);
+  if (r != hipSuccess) return fail(AMS_EHIP, std::string("cache append: ") + hipGetErrorString(r));
+  return AMS_OK;
+}
+
+size_t ams_qcache_workspace_bytes(const ams_qcache* cache, int32_t n_heads, int32_t n_tok, int32_t max_new,
+                                  int32_t max_len, int32_t n_select) {
+  std::string e;
+  if (!qcache_sizes(cache, n_heads, n_tok, max_new, max_len, n_select, e)) return 0;
+  if (n_tok == 0) return 1;
+  const ams::QAttendPlan p = qcache_plan(cache, n_heads, n_tok, max_new, max_len, n_select);
+  return align16(p.part_floats * 4) + (size_t)n_tok * cache->n_kv_heads * n_select * 4 + 1;
+}
+
+ams_status ams_qcache_attend(const ams_qcache* cache, const int32_t* tok_off, const int32_t* kv_len, int32_t n_tok,
+                             int32_t max_new, int32_t max_len, int32_t n_heads, const void* q, int64_t ldq, void* out,
+                             int64_t ldo, int32_t dtype, float scale, int32_t n_select, int32_t* selected, void* ws,
+                             size_t ws_bytes, void* stream) {
+  g_err.clear();
+  std::string e;
+  if (!qcache_sizes(cache, n_heads, n_tok, max_new, max_len, n_select, e) || !qcache_type(dtype, e))
+    return fail(AMS_EINVAL, e);
+  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(AMS_EINVAL, "scale must be finite and > 0");
+  if (selected && n_select == 0) return fail(AMS_EINVAL, "selected needs n_select > 0");
+  if (n_tok == 0) return AMS_OK;
+  const ams::QAttendPlan p = qcache_plan(cache, n_heads, n_tok, max_new, max_len, n_select);
+  max_new = std::min(max_new, n_tok);
+  const int64_t heads = (int64_t)cache->rows * n_heads * max_new;
+  if (heads > 4 * QCACHE_MAX_BLOCKS ||
+      (int64_t)cache->rows * cache->n_kv_heads * p.tiles * p.splits * (n_select ? max_new : 1) > QCACHE_MAX_BLOCKS)
+    return fail(AMS_EINVAL, "too many queries for one call: rows * max_new * n_heads is above 2^24");
+  const size_t list = (size_t)n_tok * cache->n_kv_heads * n_select * 4, part = align16(p.part_floats * 4);
+  if (!ws) return fail(AMS_EINVAL, "ws is NULL");
+  if ((uintptr_t)ws & 15) return fail(AMS_EINVAL, "ws must be 16-byte aligned");
+  if (ws_bytes < part + list + 1) return fail(AMS_ENOMEM, "workspace too small: need " + std::to_string(part + list + 1));
+  if ((uintptr_t)selected & 3) return fail(AMS_EINVAL, "selected must be 4-byte aligned");
+  int dev = 0;
+  if (int s = current_device(&dev, e)) return fail(s, e);
+  const int64_t width = (int64_t)n_heads * cache->head_dim;
+  if (!qcache_arrays(cache, tok_off, kv_len, dev, e) || !qcache_tensor(q, ldq, n_tok, width, dtype, dev, "q", e) ||
+      !qcache_tensor(out, ldo, n_tok, width, dtype, dev, "out", e) ||
+      !dev_range(ws, part + list + 1, dev, "ws", e) || (selected && !dev_range(selected, list, dev, "selected", e)))
+    return fail(AMS_EINVAL, e);
+  const ams::QCache c = qcache_view(cache);
+  const ams::QSegs sg{nullptr, tok_off, nullptr, kv_len, 0, cache->rows, n_tok, max_new};
+  hipStream_t st = (hipStream_t)stream;
+  hipError_t r = hipSuccess;
+  int32_t* sel = nullptr;
+  if (n_select) {
+    sel = selected ? selected : (int32_t*)((char*)ws + part);
+    r = ams::qcache_select(c, sg, n_heads, q, ldq, dtype, nullptr, n_select, sel, st);
+  }
+  if (r == hipSuccess)
+    r = ams::qcache_attend(c, sg, p, n_heads, q, ldq, dtype, dtype == AMS_F32, scale, nullptr, sel, n_select, out, ldo,
+                           dtype, nullptr, (float*)ws, st);
+  if (r != hipSuccess) return fail(AMS_EHIP, std::string("cache attention: ") + hipGetErrorString(r));
   return AMS_OK;
 }
 

@@ -292,6 +292,53 @@ hipError_t decode_fused(const FusedDecode& f, int grid, hipStream_t s);
 int decode_fused_grid(int device, int dh, int d);
 int fused_sync_words(int d, int H);
 
+// 8-bit K/V cache of one layer (qcache.hip): pools of n_pages pages of 64 positions,
+//   k  [page][H][64][dh], v [page][H][16][dh][4] (slot t at [t / 4][:][t % 4]) e4m3 codes
+//   ks, vs [page][H]: power-of-two scales; a code stands for its value times its page's scale
+//   kb [page][H][2][dh]: per channel the largest ceil(key / 4), then the smallest floor(key / 4), in
+//      units of the scale
+// pt [rows][ppr]: the rows' pages; entries outside [0, n_pages) hold no positions.
+struct QCache {
+  uint8_t *k, *v;
+  float *ks, *vs;
+  int8_t* kb;
+  const int32_t* pt;
+  int n_pages, H, dh, rows, ppr;
+};
+// The tokens of a call (device arrays).  Segment s: tokens off[s] .. off[s + 1] - 1 (NULL: token s) of row
+// row[s] (NULL: s), at positions pos[s].., or, with pos NULL, its last one at len[s] + len_add - 1.
+struct QSegs {
+  const int32_t *row, *off, *pos, *len;
+  int len_add, n_seg, n_tok;
+  int max_new;  // at least the longest segment (longer ones are cut to it)
+};
+// Appends the tokens' keys and values (type dt, row strides ldk / ldv, heads one after another; rope: keys
+// rotated first).  A page takes the least power-of-two scale that holds
+// its new values; one that holds older positions keeps a larger scale of theirs, and their codes are
+// rounded again when it grows.
+hipError_t qcache_append(const QCache& c, const QSegs& sg, const void* k, int64_t ldk, const void* v,
+                         int64_t ldv, int dt, const float2* rope, hipStream_t s);
+// How an attention of such a call runs (qt column tiles of 16 per wave, `keys`: the waves share them), and the
+// floats of partial sums it needs.
+struct QAttendPlan {
+  bool keys;
+  int qt, tiles, splits;
+  size_t part_floats;
+};
+QAttendPlan qcache_attend_plan(int n_seg, int n_heads, int n_kv, int dh, int n_tok, int max_new, int max_len,
+                               int n_select);
+// Causal attention of the call's tokens over what their rows hold (after their append).  pair: queries and
+// probabilities as fp16 pairs.  sel: NULL, or the pages each token attends to [n_tok][H][n_sel]
+// (increasing, then -1).  olo: the rounding errors of an fp16 output, or NULL.
+hipError_t qcache_attend(const QCache& c, const QSegs& sg, const QAttendPlan& p, int n_heads,
+                         const void* q, int64_t ldq, int dt, bool pair, float scale, const float2* rope,
+                         const int32_t* sel, int n_sel, void* o, int64_t ldo, int odt, void* olo, float* part,
+                         hipStream_t s);
+// Writes sel: the last visible page of each (token, KV head) and the n_sel - 1 others whose keys' bounds
+// promise the largest scores (ties to the lower page); all of them when n_sel or fewer are visible.
+hipError_t qcache_select(const QCache& c, const QSegs& sg, int n_heads, const void* q, int64_t ldq,
+                         int dt, const float2* rope, int n_sel, int32_t* sel, hipStream_t s);
+
 // lens[b] += add[b] (device arrays), or, when `set`, lens[b] = add[b] for the
 // rows with add[b] > 0 (a row-level rebuild leaves the other rows' lengths).
 hipError_t update_lens(int32_t* lens, const int32_t* add, int B, int set, hipStream_t s);

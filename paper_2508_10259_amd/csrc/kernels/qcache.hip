@@ -1,0 +1,1198 @@
+// The 8-bit K/V cache: append, attention and the selection of pages (kernels.h, QCache).
+//
+// Layout.  A page holds 64 positions of every head of one layer.  Keys are rows [64][D] of
+// e4m3; values are stored four positions to a dword, [16][D][4].  With keys as the A operand
+// of S^T = K Q^T and values as the A operand of O^T = V^T P^T every lane of a wave reads its
+// fragments as 16-byte loads of contiguous memory, and the probabilities leave the first
+// product in the registers the second one reads: no transposition and no LDS on the way.
+//   16x16x32 product, lane l = 16 g + i:  A row i, B column i, k slots 8 g .. 8 g + 7,
+//   C column i, rows 4 g .. 4 g + 3.
+//   S^T tile t of a 32-position step: A row i = position 16 t + i, k slots of step s = channels
+//     g D/4 + 8 s .. + 7 (both operands agree on that order); the lane gets the scores of query i
+//     at positions 16 t + 4 g + r.
+//   O^T tile j: A row i = channel i D/16 + j, k slots of group g = positions 4 g .. 4 g + 3 of
+//     tile 0, then of tile 1: one dword of the value page each, and the lane's own scores.
+// A scale is a power of two: e4m3 keeps its three mantissa bits at any exponent, so a finer scale
+// would not round better, and moving a page to a larger scale is exact but for subnormals.
+#include <type_traits>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace ams {
+
+namespace {
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int PG = KV_PAGE;
+constexpr float QC_LOG2E = 1.4426950408889634f;
+
+// A segment of the call's tokens: n tokens from t0 on, at positions p0 .. of row `row`.  Everything
+// read from the device is brought into range here, so no value of it can lead outside a buffer.
+struct Seg {
+  int row, t0, n, p0, len;
+};
+__device__ __forceinline__ Seg seg_of(const QSegs& sg, int s, int rows, int cap) {
+  Seg x;
+  x.row = sg.row ? ld_const_uniform(sg.row, s) : s;
+  x.t0 = sg.off ? ld_const_uniform(sg.off, s) : s;
+  const int t1 = sg.off ? ld_const_uniform(sg.off, s + 1) : s + 1;
+  x.t0 = min(max(x.t0, 0), sg.n_tok);
+  x.n = min(min(max(t1, x.t0), sg.n_tok) - x.t0, sg.max_new);
+  if (sg.pos) {
+    x.p0 = ld_const_uniform(sg.pos, s);
+    x.len = min(max(x.p0, -sg.n_tok) + x.n, cap);
+  } else {
+    x.len = min(max(ld_const_uniform(sg.len, s), 0) + sg.len_add, cap);
+  }
+  x.p0 = x.len - x.n;
+  if (x.row < 0 || x.row >= rows) x.n = 0;
+  return x;
+}
+
+// The pool page of a row's page `lp` (lp < ppr), -1 for one outside the pool.
+__device__ __forceinline__ int page_of(const QCache& c, int row, int lp) {
+  const int p = ld_const_uniform(c.pt, (size_t)row * c.ppr + lp);
+  return (unsigned)p < (unsigned)c.n_pages ? p : -1;
+}
+
+// A scale, at a wave-uniform index; constant while an attention runs.
+__device__ __forceinline__ float scale_of(const float* p, size_t i) {
+  return __int_as_float(ld_const_uniform((const int32_t*)p, i));
+}
+
+// Eight consecutive elements of type dt (DType) as fp32; al: their address is 16-byte aligned.
+__device__ __forceinline__ void load8(const void* p, int64_t at, int dt, bool al, float* x) {
+  if (dt == DT_F32) {
+    const float* f = (const float*)p + at;
+    if (al) {
+      *(float4*)x = *(const float4*)f;
+      *(float4*)(x + 4) = *(const float4*)(f + 4);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = f[e];
+    }
+    return;
+  }
+  uint32_t w[4];
+  const uint16_t* h = (const uint16_t*)p + at;
+  if (al) {
+    *(uint4*)w = *(const uint4*)h;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)h[2 * e] | (uint32_t)h[2 * e + 1] << 16;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (dt == DT_BF16) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+    } else {
+      const half2v v = __builtin_bit_cast(half2v, w[e]);
+      x[2 * e] = (float)v[0];
+      x[2 * e + 1] = (float)v[1];
+    }
+  }
+}
+
+// bf16 nearest even, NaN kept (the sums of an attention may be NaN).
+__device__ __forceinline__ uint32_t to_bf16(float f) { return f != f ? 0x7FC0u : f2bf(f); }
+__device__ __forceinline__ uint32_t to_f16(float f) {
+  const float c = f != f ? f : fminf(fmaxf(f, -F16_MAX), F16_MAX);
+  return __builtin_bit_cast(uint16_t, (f16)c);
+}
+
+// N (4 or 8) consecutive outputs of type dt; lo: also the rounding errors of an fp16 output.
+template <int N>
+__device__ __forceinline__ void store_row(void* p, int64_t at, int dt, bool al, const float* x, f16* lo) {
+  if (dt == DT_F32) {
+    float* f = (float*)p + at;
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {
+      if (al) *(float4*)(f + e) = float4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+      else
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[e + k] = x[e + k];
+    }
+    return;
+  }
+  uint32_t w[N / 2];
+#pragma unroll
+  for (int e = 0; e < N / 2; ++e)
+    w[e] = dt == DT_BF16 ? to_bf16(x[2 * e]) | to_bf16(x[2 * e + 1]) << 16
+                         : to_f16(x[2 * e]) | to_f16(x[2 * e + 1]) << 16;
+  uint16_t* h = (uint16_t*)p + at;
+  if (al) {
+    if (N == 8) *(uint4*)h = uint4{w[0], w[1], w[N / 2 - 2], w[N / 2 - 1]};
+    else *(uint2*)h = uint2{w[0], w[1]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) h[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+  }
+  if (lo) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const f16 hi = __builtin_bit_cast(f16, (uint16_t)(w[e / 2] >> (16 * (e & 1))));
+      lo[at + e] = sat16(x[e] - (float)hi);
+    }
+  }
+}
+
+// Eight e4m3 codes as fp16 times `scale` (a power of two).
+__device__ __forceinline__ half8 codes_f16(uint32_t a, uint32_t b, float scale) {
+  const half2v x0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)a, scale, false);
+  const half2v x1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)a, scale, true);
+  const half2v x2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, scale, false);
+  const half2v x3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, scale, true);
+  return half8{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+}
+
+__device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+__device__ __forceinline__ void unpack_codes(uint32_t w, float* x) {
+  x[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0);
+  x[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1);
+  x[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2);
+  x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
+}
+// Four codes rounded again after a multiplication by 2^de.
+__device__ __forceinline__ uint32_t rescale_codes(uint32_t w, int de) {
+  float x[4];
+  unpack_codes(w, x);
+  return pack_codes(ldexpf(x[0], de), ldexpf(x[1], de), ldexpf(x[2], de), ldexpf(x[3], de));
+}
+
+// ---------------------------------------------------------------------------
+// Append.  One workgroup per (page, head): it alone writes that page's codes, scales and bounds.
+// D/8 lanes take a token (8 channels each), a workgroup NT / (D/8) tokens at a time.  The tokens
+// stay in registers from the maximum, which sets the scale, to the rounding.
+
+// The least e >= -32 with a <= 448 2^e (448 = 0.875 * 2^9).
+__device__ __forceinline__ int scale_exponent(float a) {
+  int x;
+  const float m = frexpf(a, &x);
+  const int e = x - 9 + (m > 0.875f ? 1 : 0);
+  return a > 0.f ? min(max(e, -32), 8) : -32;
+}
+__device__ __forceinline__ int exponent_of(float scale) {
+  int x;
+  frexpf(scale, &x);
+  return x - 1;
+}
+
+struct AppendArgs {
+  QCache c;
+  QSegs sg;
+  const void *k, *v;
+  int64_t ldk, ldv;
+  int dt, alk, alv, chunks;
+  const float2* rope;
+};
+
+template <int D, int NT, int PASSES>
+__global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
+  constexpr int LPT = D / 8, TPP = NT / LPT, NW = NT / 64;
+  const QCache& c = a.c;
+  const int h = blockIdx.x % c.H, rest = blockIdx.x / c.H, chunk = rest % a.chunks, s = rest / a.chunks;
+  const Seg sg = seg_of(a.sg, s, c.rows, c.ppr * PG);
+  const int first = max(sg.p0, 0);  // tokens at positions below 0 have no place
+  if (sg.n <= 0 || sg.len <= first) return;
+  const int lp = first / PG + chunk;
+  if (lp * PG >= sg.len) return;
+  const int page = page_of(c, sg.row, lp);
+  if (page < 0) return;
+  const int s0 = max(first - lp * PG, 0), s1 = min(sg.len - lp * PG, PG), cnt = s1 - s0;
+  const int tok = sg.t0 + (lp * PG + s0 - sg.p0);  // token at slot s0
+  const int tid = threadIdx.x, sub = tid % LPT, grp = tid / LPT, lane = tid & 63, wave = tid >> 6;
+  __shared__ float red[2][NW];
+  __shared__ __align__(16) uint8_t vt[PASSES * TPP][D];
+  __shared__ float bred[2][NW][D];
+
+  float k[PASSES][8], v[PASSES][8];
+  float ka = 0.f, va = 0.f;
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int i = p * TPP + grp;
+    if (i < cnt) {
+      load8(a.k, (int64_t)(tok + i) * a.ldk + (int64_t)h * D + sub * 8, a.dt, a.alk, k[p]);
+      load8(a.v, (int64_t)(tok + i) * a.ldv + (int64_t)h * D + sub * 8, a.dt, a.alv, v[p]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k[p][e] = v[p][e] = 0.f;
+    }
+    if (a.rope) {  // pair (i, i + D/2): the partner's channels sit D/16 lanes away
+      const float2* tab = a.rope + (size_t)min(lp * PG + s0 + i, c.ppr * PG - 1) * (D / 2) + (sub % (LPT / 2)) * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float other = __shfl_xor(k[p][e], LPT / 2, 64);
+        const float2 cs = tab[e];
+        float lo, hi;
+        const bool low = sub < LPT / 2;
+        rope_pair(low ? k[p][e] : other, low ? other : k[p][e], cs.x, cs.y, lo, hi);
+        k[p][e] = low ? lo : hi;
+      }
+    }
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      nan |= k[p][e] != k[p][e] || v[p][e] != v[p][e];
+      if (k[p][e] == k[p][e]) k[p][e] = fminf(fmaxf(k[p][e], -F16_MAX), F16_MAX);
+      v[p][e] = v[p][e] == v[p][e] ? fminf(fmaxf(v[p][e], -F16_MAX), F16_MAX) : 0.f;
+      ka = fmaxf(ka, fabsf(k[p][e]));
+      va = fmaxf(va, fabsf(v[p][e]));
+    }
+    // a NaN anywhere in the token's key or value: its key gets one, its value none, so that the
+    // queries which see the token read NaN and no other query does (0 * NaN would reach those)
+    const uint64_t nans = __ballot(nan) >> (lane - lane % LPT);
+    if (sub == 0 && (nans & ((1ull << LPT) - 1ull))) k[p][0] = __uint_as_float(0x7FC00000u);
+  }
+  ka = wave_max(ka);
+  va = wave_max(va);
+  if (NW > 1) {
+    if (lane == 0) {
+      red[0][wave] = ka;
+      red[1][wave] = va;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      ka = fmaxf(ka, red[0][w]);
+      va = fmaxf(va, red[1][w]);
+    }
+  }
+  const size_t ph = (size_t)page * c.H + h;
+  int ke = scale_exponent(ka), ve = scale_exponent(va), kd = 0, vd = 0;  // kd, vd: older codes' shift (<= 0)
+  if (s0 > 0) {
+    const int ko = exponent_of(c.ks[ph]), vo = exponent_of(c.vs[ph]);
+    ke = max(ke, ko);
+    ve = max(ve, vo);
+    kd = ko - ke;
+    vd = vo - ve;
+  }
+
+  uint8_t* kpage = c.k + ph * (PG * D);
+  uint32_t* vpage = (uint32_t*)(c.v + ph * (PG * D));
+  if (kd < 0) {
+    for (int i = tid; i < s0 * (D / 8); i += NT) {
+      uint2* w = (uint2*)kpage + i;
+      const uint2 x = *w;
+      *w = uint2{rescale_codes(x.x, kd), rescale_codes(x.y, kd)};
+    }
+  }
+  float hi[8], lo[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    hi[e] = -INFINITY;
+    lo[e] = INFINITY;
+  }
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int i = p * TPP + grp;
+    if (i < cnt) {
+      uint2 w;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k[p][e] = ldexpf(k[p][e], -ke);
+      w.x = pack_codes(k[p][0], k[p][1], k[p][2], k[p][3]);
+      w.y = pack_codes(k[p][4], k[p][5], k[p][6], k[p][7]);
+      *(uint2*)(kpage + (s0 + i) * D + sub * 8) = w;
+      float x[8];
+      unpack_codes(w.x, x);
+      unpack_codes(w.y, x + 4);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {  // (a NaN code counts in no bound)
+        hi[e] = fmaxf(hi[e], x[e]);
+        lo[e] = fminf(lo[e], x[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[p][e] = ldexpf(v[p][e], -ve);
+      w.x = pack_codes(v[p][0], v[p][1], v[p][2], v[p][3]);
+      w.y = pack_codes(v[p][4], v[p][5], v[p][6], v[p][7]);
+      *(uint2*)(&vt[i][sub * 8]) = w;
+    }
+  }
+  // the channels' bounds over the workgroup's tokens
+#pragma unroll
+  for (int o = LPT; o < 64; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      hi[e] = fmaxf(hi[e], __shfl_xor(hi[e], o, 64));
+      lo[e] = fminf(lo[e], __shfl_xor(lo[e], o, 64));
+    }
+  if (NW > 1 && lane < LPT)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      bred[0][wave][sub * 8 + e] = hi[e];
+      bred[1][wave][sub * 8 + e] = lo[e];
+    }
+  __syncthreads();
+  if (tid < LPT) {
+    int8_t* b = c.kb + ph * (2 * D) + sub * 8;
+    __align__(8) int8_t bh[8], bl[8];
+    if (s0 > 0) {
+      *(uint2*)bh = *(const uint2*)b;
+      *(uint2*)bl = *(const uint2*)(b + D);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (NW > 1)
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          hi[e] = fmaxf(hi[e], bred[0][w][sub * 8 + e]);
+          lo[e] = fminf(lo[e], bred[1][w][sub * 8 + e]);
+        }
+      float nh = ceilf(hi[e] * 0.25f), nl = floorf(lo[e] * 0.25f);
+      if (s0 > 0) {
+        nh = fmaxf(nh, ceilf(ldexpf((float)bh[e], kd)));
+        nl = fminf(nl, floorf(ldexpf((float)bl[e], kd)));
+      }
+      bh[e] = (int8_t)fmaxf(nh, -128.f);
+      bl[e] = (int8_t)fminf(nl, 127.f);
+    }
+    *(uint2*)b = *(uint2*)bh;
+    *(uint2*)(b + D) = *(uint2*)bl;
+  }
+  // the values, four slots to a dword, 4 channels to a 16-byte store; slots that this call does not
+  // write keep their codes (older ones moved to the new scale)
+  const int q0 = vd < 0 ? 0 : s0 / 4, q1 = (s1 + 3) / 4;
+  for (int i = tid; i < (q1 - q0) * (D / 4); i += NT) {
+    const int quad = q0 + i / (D / 4), ch = i % (D / 4) * 4;
+    uint32_t r[4] = {0u, 0u, 0u, 0u};  // the quad's slots: 4 channels each
+    uint32_t fresh = 0u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int slot = quad * 4 + e;
+      if (slot >= s0 && slot < s1) {
+        r[e] = *(const uint32_t*)&vt[slot - s0][ch];
+        fresh |= 0xFFu << (8 * e);
+      }
+    }
+    const uint32_t t0 = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), t1 = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);
+    const uint32_t t2 = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u), t3 = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+    uint4 w{__builtin_amdgcn_perm(t2, t0, 0x05040100u), __builtin_amdgcn_perm(t2, t0, 0x07060302u),
+            __builtin_amdgcn_perm(t3, t1, 0x05040100u), __builtin_amdgcn_perm(t3, t1, 0x07060302u)};
+    uint4* dst = (uint4*)(vpage + quad * D + ch);
+    if (fresh != 0xFFFFFFFFu) {
+      const uint4 old = *dst;
+      uint32_t ow[4] = {old.x, old.y, old.z, old.w}, *nw = (uint32_t*)&w;
+      uint32_t older = 0u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (quad * 4 + e < s0) older |= 0xFFu << (8 * e);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (vd < 0) ow[e] = (rescale_codes(ow[e], vd) & older) | (ow[e] & ~older);
+        nw[e] = (nw[e] & fresh) | (ow[e] & ~fresh);
+      }
+    }
+    *dst = w;
+  }
+  if (tid == 0) {
+    c.ks[ph] = ldexpf(1.f, ke);
+    c.vs[ph] = ldexpf(1.f, ve);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention.  A query's column c of a segment is head c % G of the KV head's group at token c / G.
+// A wave keeps QT tiles of 16 columns and walks 32-position steps, with the running maximum and sum
+// of each column in the lanes that hold it.  KEYS: the four waves share the columns and deal the
+// steps among them (few columns, the cache streams once); otherwise each wave has its own columns and
+// all walk the same steps (many columns; K/V come from the L1 for three waves of four).
+// PAIR (fp32 queries): queries and probabilities as fp16 pairs, about 22 bits.
+
+struct AttendArgs {
+  QCache c;
+  QSegs sg;
+  const void* q;
+  int64_t ldq;
+  void* o;
+  int64_t ldo;
+  f16* olo;
+  int dt, odt, alq, alo, G;
+  float scale;
+  const float2* rope;
+  const int32_t* sel;  // [n_tok][H][n_sel] pages of a token's row (SEL)
+  int n_sel, tiles, splits;
+  float* part;
+};
+
+template <int D> struct Step {  // a lane's K and V bytes of 32 positions
+  uint4 k[2][D / 64], v[2][D / 64];
+};
+
+template <int D, bool NT>
+__device__ __forceinline__ void load_k(const QCache& c, size_t ph, int half, int lane, uint4 (&k)[2][D / 64]) {
+  const uint8_t* p = c.k + ph * (PG * D) + half * (32 * D) + (lane & 15) * D + (lane >> 4) * (D / 4);
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) {
+      const void* a = p + t * 16 * D + e * 16;
+      k[t][e] = NT ? ld_stream(a) : *(const uint4*)a;
+    }
+}
+template <int D, bool NT>
+__device__ __forceinline__ void load_v(const QCache& c, size_t ph, int half, int lane, uint4 (&v)[2][D / 64]) {
+  const uint8_t* p = c.v + ph * (PG * D) + half * (32 * D) + (lane >> 4) * (4 * D) + (lane & 15) * (D / 4);
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) {
+      const void* a = p + t * 16 * D + e * 16;
+      v[t][e] = NT ? ld_stream(a) : *(const uint4*)a;
+    }
+}
+
+template <int D, int QT, bool PAIR, bool KEYS, bool SEL>
+__global__ __launch_bounds__(256) void k_qcache_attend(AttendArgs a) {
+  constexpr int NS = D / 32, NJ = D / 16, CT = 16 * QT;
+  const QCache& c = a.c;
+  // block -> (split, column tile, head, segment[, token])
+  int id = blockIdx.x;
+  int split, tile, h, s, tokn = 0;
+  if (KEYS) {
+    split = id % a.splits; id /= a.splits;
+    h = id % c.H; id /= c.H;
+    tile = id % a.tiles; id /= a.tiles;
+    if (SEL) { tokn = id % a.sg.max_new; id /= a.sg.max_new; }
+    s = id;
+  } else {
+    // the tiles of one (segment, head) pair follow each other on one XCD (blocks go to the 8 XCDs in
+    // turn), the longest first: they read the same pages through that XCD's L2
+    const int x = id & 7; id >>= 3;
+    split = id % a.splits; id /= a.splits;
+    tile = a.tiles - 1 - id % a.tiles; id /= a.tiles;
+    const int pair = id * 8 + x;
+    if (pair >= a.sg.n_seg * c.H) return;
+    h = pair % c.H;
+    s = pair / c.H;
+  }
+  Seg sg = seg_of(a.sg, s, c.rows, c.ppr * PG);
+  if (SEL) {  // one token of the segment
+    if (tokn >= sg.n) return;
+    sg.t0 += tokn;
+    sg.p0 += tokn;
+    sg.n = 1;
+  }
+  const int G = a.G, ncols = sg.n * G;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int blockcol = tile * (KEYS ? CT : 4 * CT);
+  if (blockcol >= ncols) return;
+  const int col0 = KEYS ? blockcol : blockcol + wave * CT;
+
+  // queries: scaled by a power of two so that a column's largest element is in [2^10, 2^11)
+  half8 qh[QT][NS], ql[PAIR ? QT : 1][NS];
+  float cq[QT];
+  int vis[QT], tokc[QT], headc[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int col = col0 + 16 * t + i;
+    const bool ok = col < ncols;
+    tokc[t] = ok ? col / G : 0;
+    headc[t] = h * G + (ok ? col % G : 0);
+    vis[t] = ok ? sg.p0 + tokc[t] + 1 : 0;
+    tokc[t] = ok ? sg.t0 + tokc[t] : -1;
+    float x[NS][8], m = 0.f;
+#pragma unroll
+    for (int k = 0; k < NS; ++k) {
+      if (ok) load8(a.q, (int64_t)tokc[t] * a.ldq + (int64_t)headc[t] * D + g * (D / 4) + k * 8, a.dt, a.alq, x[k]);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[k][e] = 0.f;
+    }
+    if (a.rope) {
+      const float2* tab = a.rope + (size_t)min(max(vis[t] - 1, 0), c.ppr * PG - 1) * (D / 2) + (g & 1) * (D / 4);
+#pragma unroll
+      for (int k = 0; k < NS; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float other = __shfl_xor(x[k][e], 32, 64);
+          const float2 cs = tab[k * 8 + e];
+          float lo, hi;
+          rope_pair(g < 2 ? x[k][e] : other, g < 2 ? other : x[k][e], cs.x, cs.y, lo, hi);
+          x[k][e] = g < 2 ? lo : hi;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < NS; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[k][e]));
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    int ex;
+    frexpf(m, &ex);
+    if (!(m > 0.f)) ex = 0;
+    cq[t] = ldexpf(a.scale * QC_LOG2E, ex - 11);
+#pragma unroll
+    for (int k = 0; k < NS; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y = ldexpf(x[k][e], 11 - ex);
+        qh[t][k][e] = (f16)y;
+        if (PAIR) ql[t][k][e] = (f16)(y - (float)qh[t][k][e]);
+      }
+  }
+  // the columns' first and last visible positions of this wave
+  int vmin = 0x7FFFFFFF, vmax = 0;
+#pragma unroll
+  for (int t = 0; t < QT; ++t)
+    if (tokc[t] >= 0) {
+      vmin = min(vmin, vis[t]);
+      vmax = max(vmax, vis[t]);
+    }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {
+    vmin = min(vmin, __shfl_xor(vmin, o, 64));
+    vmax = max(vmax, __shfl_xor(vmax, o, 64));
+  }
+  vmin = __builtin_amdgcn_readfirstlane(vmin);
+  vmax = __builtin_amdgcn_readfirstlane(vmax);
+
+  // 32-position steps of this split, and of this wave
+  const int32_t* list = SEL ? a.sel + ((size_t)sg.t0 * c.H + h) * a.n_sel : nullptr;
+  int steps;
+  if (SEL) {
+    int lo = 0, up = a.n_sel;  // the entries before the first -1
+    while (lo < up) {
+      const int mid = (lo + up) >> 1;
+      if (ld_const_uniform(list, mid) >= 0) lo = mid + 1;
+      else up = mid;
+    }
+    steps = 2 * lo;
+  } else {
+    // (in KEYS mode every wave has the same columns; otherwise each stops at its own last position)
+    steps = (vmax + 31) / 32;
+  }
+  int all = steps;
+  if (!KEYS) {  // splits are the same for the workgroup's waves
+    const int lastcol = min(blockcol + 4 * CT, ncols) - 1;
+    all = (max(sg.p0 + lastcol / G + 1, 0) + 31) / 32;
+  }
+  const int per = (all + a.splits - 1) / a.splits;
+  const int begin = split * per, end = min(steps, begin + per), inc = KEYS ? 4 : 1;
+
+  f32x4 o[QT][NJ];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // o is in units of 2^vref: a value page's scale relative to it goes into the conversion of its codes
+  int vref = 0;
+  bool first = true;
+
+  // the next step with a page in the pool: its page index and half
+  auto find = [&](int& st, size_t& ph, int& pos) {
+    for (; st < end; st += inc) {
+      int lp = st >> 1;
+      if (SEL) lp = ld_const_uniform(list, lp);
+      if (SEL && (unsigned)lp >= (unsigned)c.ppr) continue;
+      const int page = page_of(c, sg.row, lp);
+      if (page < 0) continue;
+      ph = (size_t)page * c.H + h;
+      pos = lp * PG + 32 * (st & 1);
+      if (pos >= vmax) continue;  // the last page's second half
+      return true;
+    }
+    return false;
+  };
+
+  Step<D> x;
+  int st = begin + (KEYS ? wave : 0), pos = 0;
+  size_t ph = 0;
+  bool more = find(st, ph, pos);
+  if (more) {
+    load_k<D, KEYS>(c, ph, (pos >> 5) & 1, lane, x.k);
+    load_v<D, KEYS>(c, ph, (pos >> 5) & 1, lane, x.v);
+  }
+  // One step; EDGE: some of its positions are masked for a column, or lie behind the row's last one.
+  auto step = [&](auto edge_tag) {
+    constexpr bool EDGE = decltype(edge_tag)::value;
+    const float ks = scale_of(c.ks, ph), vs = scale_of(c.vs, ph);
+    const int p0 = pos;
+    int nst = st + inc, npos = 0;
+    size_t nph = 0;
+    const bool nmore = find(nst, nph, npos);
+    // S^T = K Q^T
+    f32x4 sc[QT][2];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) sc[t][0] = sc[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int k = 0; k < NS; ++k) {
+        const uint4 w = x.k[n][k / 2];
+        const half8 A = k & 1 ? codes_f16(w.z, w.w, 1.f) : codes_f16(w.x, w.y, 1.f);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          sc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, qh[t][k], sc[t][n], 0, 0, 0);
+          if (PAIR) sc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, ql[t][k], sc[t][n], 0, 0, 0);
+        }
+      }
+    if (nmore) load_k<D, KEYS>(c, nph, (npos >> 5) & 1, lane, x.k);
+    // softmax of the 32 positions
+    int ve = exponent_of(vs);
+    if (first) vref = ve;
+    first = false;
+    float fall = 1.f;  // o to another unit where the page's scale is far from it
+    if (ve - vref > 4 || ve - vref < -6) {
+      fall = ldexpf(1.f, vref - ve);
+      vref = ve;
+    }
+    const float vr = ldexpf(1.f, ve - vref);
+    half8 ph8[QT], pl8[PAIR ? QT : 1];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const float cs = fmaxf(cq[t] * ks, 1e-37f);  // (not 0: -inf stays -inf)
+      float top = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (EDGE && p0 + 16 * n + 4 * g + r >= vis[t]) sc[t][n][r] = -INFINITY;
+          top = fmaxf(top, sc[t][n][r]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float nm = fmaxf(m[t], top * cs);
+      // probabilities times 2^12: fp16 keeps them to full precision down to 2^-26 of the largest
+      const float base = nm == -INFINITY ? 0.f : nm - 12.f;
+      if (__any(nm > m[t]) || fall != 1.f) {
+        const float al = nm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - nm);
+        l[t] *= al;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) o[t][j] *= al * fall;
+        m[t] = nm;
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(sc[t][n][r], cs, -base));
+          l[t] += p;
+          ph8[t][4 * n + r] = (f16)p;
+          if (PAIR) pl8[t][4 * n + r] = (f16)(p - (float)ph8[t][4 * n + r]);
+        }
+    }
+    // O^T += V^T P^T; codes behind the row's last position may be anything
+    if (EDGE) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int left = min(max(sg.len - (p0 + 16 * n + 4 * g), 0), 4);
+        const uint32_t keep = left == 4 ? 0xFFFFFFFFu : (1u << (8 * left)) - 1u;
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) {
+          x.v[n][e].x &= keep;
+          x.v[n][e].y &= keep;
+          x.v[n][e].z &= keep;
+          x.v[n][e].w &= keep;
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const uint4 w0 = x.v[0][j / 4], w1 = x.v[1][j / 4];
+      const uint32_t d0 = j % 4 == 0 ? w0.x : j % 4 == 1 ? w0.y : j % 4 == 2 ? w0.z : w0.w;
+      const uint32_t d1 = j % 4 == 0 ? w1.x : j % 4 == 1 ? w1.y : j % 4 == 2 ? w1.z : w1.w;
+      const half8 A = codes_f16(d0, d1, vr);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, ph8[t], o[t][j], 0, 0, 0);
+        if (PAIR) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, pl8[t], o[t][j], 0, 0, 0);
+      }
+    }
+    if (nmore) load_v<D, KEYS>(c, nph, (npos >> 5) & 1, lane, x.v);
+    st = nst;
+    ph = nph;
+    pos = npos;
+    more = nmore;
+  };
+  // (positions increase, so the steps at the edge are the last ones; vmin <= len)
+  while (more && pos + 32 <= vmin) step(std::false_type{});
+  while (more) step(std::true_type{});
+  const float unit = ldexpf(1.f, vref);
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    l[t] += __shfl_xor(l[t], 16, 64);
+    l[t] += __shfl_xor(l[t], 32, 64);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) o[t][j] *= unit;
+  }
+
+  constexpr int LD = D + 4;
+  if (KEYS) {  // the four waves' sums meet in LDS
+    // (32 columns: in two rounds, since four waves' sums take more than 64 KB)
+    constexpr int SLOTS = QT == 1 ? 4 : 2;
+    __shared__ __align__(16) float so[KEYS ? SLOTS * CT * LD : 4];
+    __shared__ float sm[4][CT], sl[4][CT];
+    const int live = min(ncols - blockcol, CT);
+    if (g == 0)
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        sm[wave][16 * t + i] = m[t];
+        sl[wave][16 * t + i] = l[t];
+      }
+    __syncthreads();
+    auto put = [&](int slot) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+        if (16 * t + i < live)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < NJ; j += 4)
+              *(f32x4*)&so[(slot * CT + 16 * t + i) * LD + (4 * g + r) * NJ + j] =
+                  f32x4{o[t][j][r], o[t][j + 1][r], o[t][j + 2][r], o[t][j + 3][r]};
+    };
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) M = fmaxf(M, sm[w][16 * t + i]);
+      const float f = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - M);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) o[t][j] *= f;
+    }
+    if (SLOTS == 4) {
+      put(wave);
+    } else {
+      if (wave >= 2) put(wave - 2);
+      __syncthreads();
+      if (wave < 2)
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+          if (16 * t + i < live)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int j = 0; j < NJ; ++j) o[t][j][r] += so[(wave * CT + 16 * t + i) * LD + (4 * g + r) * NJ + j];
+      // each of the two waves writes where it alone has read
+      if (wave < 2) put(wave);
+    }
+    __syncthreads();
+    for (int k = tid; k < live * (D / 4); k += 256) {
+      const int cc = k / (D / 4), ch = k % (D / 4) * 4;
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) M = fmaxf(M, sm[w][cc]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) L += sm[w][cc] == -INFINITY ? 0.f : sl[w][cc] * __builtin_amdgcn_exp2f(sm[w][cc] - M);
+      f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < SLOTS; ++w) y += *(const f32x4*)&so[(w * CT + cc) * LD + ch];
+      const int col = blockcol + cc, tok = sg.t0 + col / G, head = h * G + col % G;
+      if (a.splits == 1) {
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+        store_row<4>(a.o, (int64_t)tok * a.ldo + (int64_t)head * D + ch, a.odt, a.alo, z, a.olo);
+      } else {
+        float* p = a.part + (((size_t)tok * (c.H * G) + head) * a.splits + split) * LD;
+        *(f32x4*)(p + ch) = y;
+        if (ch == 0) {
+          p[D] = M;
+          p[D + 1] = L;
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      if (tokc[t] < 0) continue;
+      if (a.splits == 1) {
+        const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float z[NJ];
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) z[j] = o[t][j][r] * inv;
+          store_row<NJ>(a.o, (int64_t)tokc[t] * a.ldo + (int64_t)headc[t] * D + (4 * g + r) * NJ, a.odt, a.alo, z, a.olo);
+        }
+      } else {
+        float* p = a.part + (((size_t)tokc[t] * (c.H * G) + headc[t]) * a.splits + split) * LD;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < NJ; j += 4)
+            *(f32x4*)(p + (4 * g + r) * NJ + j) = f32x4{o[t][j][r], o[t][j + 1][r], o[t][j + 2][r], o[t][j + 3][r]};
+        if (g == 0) {
+          p[D] = m[t];
+          p[D + 1] = l[t];
+        }
+      }
+    }
+  }
+}
+
+// Joins the splits of each (token, head): a wave each, in split order.
+template <int D>
+__global__ __launch_bounds__(256) void k_qcache_join(AttendArgs a) {
+  constexpr int LD = D + 4, E = D / 64;
+  const int heads = a.c.H * a.G, lane = threadIdx.x & 63;
+  const int item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int head = item % heads, rest = item / heads, tokn = rest % a.sg.max_new, s = rest / a.sg.max_new;
+  if (s >= a.sg.n_seg) return;
+  const Seg sg = seg_of(a.sg, __builtin_amdgcn_readfirstlane(s), a.c.rows, a.c.ppr * PG);
+  if (tokn >= sg.n) return;
+  const int tok = sg.t0 + tokn;
+  const float* p = a.part + ((size_t)tok * heads + head) * a.splits * LD;
+  float M = -INFINITY;
+  for (int k = lane; k < a.splits; k += 64) M = fmaxf(M, p[(size_t)k * LD + D]);
+  M = wave_max(M);
+  float L = 0.f, y[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = 0.f;
+  for (int k = 0; k < a.splits; ++k) {
+    const float* q = p + (size_t)k * LD;
+    const float mk = q[D], f = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk - M);
+    L += q[D + 1] * f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] += q[lane * E + e] * f;
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  const int64_t at = (int64_t)tok * a.ldo + (int64_t)head * D + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float z = y[e] * inv;
+    if (a.odt == DT_F32) ((float*)a.o)[at + e] = z;
+    else if (a.odt == DT_BF16) ((uint16_t*)a.o)[at + e] = (uint16_t)to_bf16(z);
+    else {
+      const uint16_t w = (uint16_t)to_f16(z);
+      ((uint16_t*)a.o)[at + e] = w;
+      if (a.olo) a.olo[at + e] = sat16(z - (float)__builtin_bit_cast(f16, w));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Selection.  A workgroup per (token, KV head).  The score of a page is an upper bound of q . k over
+// its keys, from each channel's largest and smallest key, in whole numbers (|q^| <= 127 times bounds of
+// at most 112, 128 channels: below 2^21), so it has the same bits in any order of summation:
+//   2^ke max over heads of sum_d max(q^_d, 0) hi_d + min(q^_d, 0) lo_d
+// as one 8-bit product of [q^+ | q^-] (a head per column) with the bounds' rows [hi | lo] (a page per row).
+// Then the n_sel best: the threshold by four 8-bit digits of the keys' order, ties to the lower page.
+
+struct SelectArgs {
+  QCache c;
+  QSegs sg;
+  const void* q;
+  int64_t ldq;
+  int dt, alq, G, n_sel;
+  const float2* rope;
+  int32_t* sel;
+};
+
+constexpr int SEL_OUT = 0;  // the key of a page that cannot be chosen; every other key is larger
+
+template <int D, int NT>
+__global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
+  constexpr int NW = NT / 64, NB = 2 * D / 64;
+  extern __shared__ uint32_t key[];  // [ppr]
+  __shared__ uint32_t hist[256];
+  __shared__ uint32_t pick[2];
+  __shared__ uint32_t wsum[2][NW];
+  const QCache& c = a.c;
+  int id = blockIdx.x;
+  const int h = id % c.H;
+  id /= c.H;
+  const int tokn = id % a.sg.max_new, s = id / a.sg.max_new;
+  const Seg sg = seg_of(a.sg, s, c.rows, c.ppr * PG);
+  if (tokn >= sg.n) return;
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tok = sg.t0 + tokn, vis = max(sg.p0 + tokn + 1, 0), np = (vis + PG - 1) / PG, G = a.G;
+  int32_t* out = a.sel + ((size_t)tok * c.H + h) * a.n_sel;
+
+  if (np > a.n_sel) {
+    // the largest |q| of the group's heads; lane (i, g) reads head i's channels 64 b + 16 g .. of each
+    // block b of 64 (all waves the same)
+    auto load16 = [&](int col, int b, float* x) {
+      const int64_t at = (int64_t)tok * a.ldq + (int64_t)(h * G + col) * D + (64 * b + 16 * g) % D;
+      load8(a.q, at, a.dt, a.alq, x);
+      load8(a.q, at + 8, a.dt, a.alq, x + 8);
+      if (a.rope) {
+        const int d0 = (64 * b + 16 * g) % D;
+        const bool low = d0 < D / 2;
+        float y[16];
+        load8(a.q, at + (low ? D / 2 : -D / 2), a.dt, a.alq, y);
+        load8(a.q, at + (low ? D / 2 : -D / 2) + 8, a.dt, a.alq, y + 8);
+        const float2* tab = a.rope + (size_t)min(max(vis - 1, 0), c.ppr * PG - 1) * (D / 2) + d0 % (D / 2);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float lo, hi;
+          rope_pair(low ? x[e] : y[e], low ? y[e] : x[e], tab[e].x, tab[e].y, lo, hi);
+          x[e] = low ? lo : hi;
+        }
+      }
+    };
+    float m = 0.f;
+    for (int col = i; col < G; col += 16)
+#pragma unroll
+      for (int b = 0; b < D / 64; ++b) {
+        float x[16];
+        load16(col, b, x);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[e]));
+      }
+    m = wave_max(m);
+    int ex;
+    frexpf(m, &ex);
+    const bool flat = !(m > 0.f) || m == INFINITY;  // nothing to rank by: every score 0
+    for (int c0 = 0; c0 < G; c0 += 16) {
+      const int col = c0 + i;
+      i32x4 B[NB];
+#pragma unroll
+      for (int b = 0; b < D / 64; ++b) {
+        float x[16];
+        if (col < G && !flat) load16(col, b, x);
+        else
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = 0.f;
+        i32x4 up = {0, 0, 0, 0}, dn = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float f = x[e] == x[e] ? rintf(ldexpf(x[e], 7 - ex)) : 0.f;
+          const int v = (int)fminf(fmaxf(f, -127.f), 127.f);
+          up[e / 4] |= (max(v, 0) & 255) << (8 * (e % 4));
+          dn[e / 4] |= (min(v, 0) & 255) << (8 * (e % 4));
+        }
+        B[b] = up;
+        B[b + D / 64] = dn;
+      }
+      for (int p0 = wave * 16; p0 < np; p0 += NW * 16) {
+        const int lp = p0 + i;
+        int page = -1;
+        if (lp < np) {
+          page = c.pt[(size_t)sg.row * c.ppr + lp];
+          if ((unsigned)page >= (unsigned)c.n_pages) page = -1;
+        }
+        i32x4 acc = {0, 0, 0, 0};
+        float ks = 0.f;
+        i32x4 A[NB];
+        if (page >= 0) {
+          const size_t ph = (size_t)page * c.H + h;
+          ks = c.ks[ph];
+          const i32x4* b = (const i32x4*)(c.kb + ph * (2 * D)) + g;
+#pragma unroll
+          for (int n = 0; n < NB; ++n) A[n] = b[4 * n];
+        } else {
+#pragma unroll
+          for (int n = 0; n < NB; ++n) A[n] = i32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(A[n], B[n], acc, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          int v = col < G ? acc[r] : INT_MIN;
+#pragma unroll
+          for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor(v, o, 64));
+          const float sk = __shfl(ks, 4 * g + r, 64);
+          const int there = __shfl(page, 4 * g + r, 64);
+          const int lpr = p0 + 4 * g + r;
+          if (i == 0 && lpr < np) {
+            uint32_t u = __float_as_uint((float)v * sk);
+            if (u == 0x80000000u) u = 0u;
+            u = u & 0x80000000u ? ~u : u | 0x80000000u;
+            if (lpr == np - 1) u = 0xFFFFFFFFu;
+            if (there < 0) u = SEL_OUT;
+            key[lpr] = c0 ? max(key[lpr], u) : u;
+          }
+        }
+      }
+    }
+    __syncthreads();
+    // the key of rank n_sel: digit by digit, `need` of the keys with the digits so far are wanted
+    uint32_t prefix = 0u, need = a.n_sel;
+    for (int d = 24; d >= 0; d -= 8) {
+      for (int b = tid; b < 256; b += NT) hist[b] = 0u;
+      __syncthreads();
+      for (int p = tid; p < np; p += NT) {
+        const uint32_t u = key[p];
+        if (d == 24 || (u >> (d + 8)) == (prefix >> (d + 8))) atomicAdd(&hist[(u >> d) & 255u], 1u);
+      }
+      __syncthreads();
+      if (wave == 0) {  // lane l: digits 255 - 4 l .. 252 - 4 l; the sums from the top down
+        uint32_t n[4], t = 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          n[e] = hist[255 - 4 * lane - e];
+          t += n[e];
+        }
+        uint32_t above = t;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const uint32_t y = __shfl_up(above, o, 64);
+          if (lane >= o) above += y;
+        }
+        above -= t;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (above < need && need <= above + n[e]) {
+            pick[0] = prefix | (uint32_t)(255 - 4 * lane - e) << d;
+            pick[1] = need - above;
+          }
+          above += n[e];
+        }
+      }
+      __syncthreads();
+      prefix = pick[0];
+      need = pick[1];
+    }
+    // a thread takes consecutive pages: counts of larger and of equal keys, then their places in order
+    const int each = (np + NT - 1) / NT, b0 = min(tid * each, np), b1 = min(b0 + each, np);
+    uint32_t more = 0u, same = 0u;
+    for (int p = b0; p < b1; ++p) {
+      more += key[p] > prefix;
+      same += key[p] == prefix;
+    }
+    uint32_t im = more, is = same;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t y = __shfl_up(im, o, 64), z = __shfl_up(is, o, 64);
+      if (lane >= o) {
+        im += y;
+        is += z;
+      }
+    }
+    if (lane == 63) {
+      wsum[0][wave] = im;
+      wsum[1][wave] = is;
+    }
+    __syncthreads();
+    uint32_t pm = im - more, ps = is - same;
+    for (int w = 0; w < wave; ++w) {
+      pm += wsum[0][w];
+      ps += wsum[1][w];
+    }
+    const bool real = prefix != SEL_OUT;  // fewer pages than n_sel can be chosen otherwise
+    for (int p = b0; p < b1; ++p) {
+      const uint32_t u = key[p];
+      const bool eq = u == prefix;
+      if (u > prefix || (eq && real && ps < need)) out[pm + (real ? min(ps, need) : 0u)] = p;
+      pm += u > prefix;
+      ps += eq;
+    }
+    if (!real) {
+      uint32_t total = 0u;
+      for (int w = 0; w < NW; ++w) total += wsum[0][w];
+      for (int p = (int)total + tid; p < a.n_sel; p += NT) out[p] = -1;
+    }
+    return;
+  }
+  // every page in view: the ones in the pool, in order
+  if (wave == 0) {
+    int at = 0;
+    for (int p0 = 0; p0 < np; p0 += 64) {
+      const int p = p0 + lane;
+      const bool ok = p < np && (unsigned)c.pt[(size_t)sg.row * c.ppr + p] < (unsigned)c.n_pages;
+      const uint64_t b = __ballot(ok);
+      if (ok) out[at + __popcll(b & ((1ull << lane) - 1ull))] = p;
+      at += __popcll(b);
+    }
+    for (int p = at + lane; p < a.n_sel; p += 64) out[p] = -1;
+  }
+}
+
+bool aligned16(const void* p, int64_t ld, int es) { return ((uintptr_t)p & 15) == 0 && (ld * es) % 16 == 0; }
+int type_bytes(int dt) { return dt == DT_F32 ? 4 : 2; }
+
+}  // namespace
+
+hipError_t qcache_append(const QCache& c, const QSegs& sg, const void* k, int64_t ldk, const void* v,
+                         int64_t ldv, int dt, const float2* rope, hipStream_t s) {
+  AppendArgs a{c, sg, k, v, ldk, ldv, dt, aligned16(k, ldk, type_bytes(dt)), aligned16(v, ldv, type_bytes(dt)), 0, rope};
+  const int max_new = sg.max_new;
+  // n tokens touch at most (n + 62) / 64 + 1 pages
+  a.chunks = (max_new + 62) / PG + 1;
+  const unsigned grid = (unsigned)a.chunks * c.H * sg.n_seg;
+  const int few = c.dh == 128 ? 4 : 8;  // tokens that one wave takes at once
+  if (c.dh == 128) {
+    if (max_new <= few) k_qcache_append<128, 64, 1><<<grid, 64, 0, s>>>(a);
+    else k_qcache_append<128, 256, 4><<<grid, 256, 0, s>>>(a);
+  } else {
+    if (max_new <= few) k_qcache_append<64, 64, 1><<<grid, 64, 0, s>>>(a);
+    else k_qcache_append<64, 256, 2><<<grid, 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+QAttendPlan qcache_attend_plan(int n_seg, int n_heads, int n_kv, int dh, int n_tok, int max_new, int max_len,
+                               int n_select) {
+  QAttendPlan p{};
+  const int G = n_heads / n_kv;
+  const int64_t cols = n_select ? G : (int64_t)max_new * G;
+  p.keys = n_select > 0 || cols <= 32;
+  p.qt = p.keys ? (cols <= 16 || n_select ? 1 : 2) : 2;
+  const int per = p.keys ? 16 * p.qt : 64 * p.qt;
+  p.tiles = (int)((cols + per - 1) / per);
+  // Splits: the last 32-position step of every workgroup ends at about the same time when there are
+  // some 1,024 of them (four per CU); a split keeps at least 2 steps for each of its waves.
+  const int64_t blocks = (int64_t)n_seg * n_kv * p.tiles * (n_select ? max_new : 1);
+  const int64_t positions = n_select ? (int64_t)n_select * PG : max_len;
+  const int64_t steps = (positions + 31) / 32, least = p.keys ? 8 : 16;
+  int64_t splits = (1024 + blocks - 1) / blocks;
+  splits = splits < (steps + least - 1) / least ? splits : (steps + least - 1) / least;
+  if (splits > 256) splits = 256;
+  if (splits < 1) splits = 1;
+  p.splits = (int)splits;
+  p.part_floats = splits > 1 ? (size_t)n_tok * n_heads * splits * (dh + 4) : 0;
+  return p;
+}
+
+template <int D, bool PAIR>
+static hipError_t attend_launch(const QAttendPlan& p, AttendArgs& a, hipStream_t s) {
+  const unsigned pairs = (unsigned)a.sg.n_seg * a.c.H;
+  if (a.sel) {
+    k_qcache_attend<D, 1, PAIR, true, true><<<pairs * p.tiles * p.splits * a.sg.max_new, 256, 0, s>>>(a);
+  } else if (p.keys) {
+    if (p.qt == 1) k_qcache_attend<D, 1, PAIR, true, false><<<pairs * p.tiles * p.splits, 256, 0, s>>>(a);
+    else k_qcache_attend<D, 2, PAIR, true, false><<<pairs * p.tiles * p.splits, 256, 0, s>>>(a);
+  } else {
+    k_qcache_attend<D, 2, PAIR, false, false><<<(pairs + 7) / 8 * 8 * p.tiles * p.splits, 256, 0, s>>>(a);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const size_t items = (size_t)a.sg.n_seg * a.sg.max_new * a.c.H * a.G;
+  k_qcache_join<D><<<(unsigned)((items + 3) / 4), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t qcache_attend(const QCache& c, const QSegs& sg, const QAttendPlan& p, int n_heads,
+                         const void* q, int64_t ldq, int dt, bool pair, float scale, const float2* rope,
+                         const int32_t* sel, int n_sel, void* o, int64_t ldo, int odt, void* olo, float* part,
+                         hipStream_t s) {
+  AttendArgs a{c, sg, q, ldq, o, ldo, (f16*)olo, dt, odt, aligned16(q, ldq, type_bytes(dt)),
+               aligned16(o, ldo, type_bytes(odt)), n_heads / c.H, scale, rope, sel, n_sel, p.tiles, p.splits, part};
+  if (c.dh == 128) return pair ? attend_launch<128, true>(p, a, s) : attend_launch<128, false>(p, a, s);
+  return pair ? attend_launch<64, true>(p, a, s) : attend_launch<64, false>(p, a, s);
+}
+
+template <int D, int NT>
+static hipError_t select_launch(const SelectArgs& a, unsigned grid, hipStream_t s) {
+  const size_t lds = (size_t)a.c.ppr * 4;
+  if (lds > 60 * 1024) {  // above 64 KB with the kernel's own
+    hipError_t e = hipFuncSetAttribute((const void*)k_qcache_select<D, NT>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  k_qcache_select<D, NT><<<grid, NT, lds, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t qcache_select(const QCache& c, const QSegs& sg, int n_heads, const void* q, int64_t ldq,
+                         int dt, const float2* rope, int n_sel, int32_t* sel, hipStream_t s) {
+  SelectArgs a{c, sg, q, ldq, dt, aligned16(q, ldq, type_bytes(dt)), n_heads / c.H, n_sel, rope, sel};
+  const unsigned grid = (unsigned)sg.n_seg * c.H * sg.max_new;
+  if (c.ppr <= 256)
+    return c.dh == 128 ? select_launch<128, 256>(a, grid, s) : select_launch<64, 256>(a, grid, s);
+  return c.dh == 128 ? select_launch<128, 1024>(a, grid, s) : select_launch<64, 1024>(a, grid, s);
+}
+
+}  // namespace ams

@@ -1,0 +1,444 @@
+"""The 8-bit K/V cache on the device against the 64-bit reference: every byte of an append, attention
+within tolerances derived from its roundings, every selected page.
+
+Pools start as arbitrary bytes (NaN codes among them): only what an append wrote may matter.
+"""
+import math
+
+import numpy as np
+import pytest
+
+import oracle.qcache as Q
+
+pytestmark = pytest.mark.gpu
+
+HALF_STEP = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def dtype_of(name):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+class Both:
+    """One cache on the device and in the reference, rows over a shuffled pool."""
+
+    def __init__(self, rows, ppr, H, D, seed=0, spare=2, table=None):
+        import torch
+        from paper_2508_10259_amd.qcache import E4M3, QuantCache
+        self.rng = rng = np.random.default_rng(seed)
+        self.rows, self.ppr, self.H, self.D = rows, ppr, H, D
+        P = rows * ppr + spare
+        if table is None:
+            table = rng.permutation(P)[:rows * ppr].reshape(rows, ppr)
+        table = np.asarray(table, np.int32)
+        k = rng.integers(0, 256, (P, H, 64, D), dtype=np.uint8)
+        v = rng.integers(0, 256, (P, H, 16, D, 4), dtype=np.uint8)
+        ks, vs = np.full((P, H), 2.0 ** 5, np.float32), np.full((P, H), 2.0 ** -30, np.float32)
+        b = rng.integers(-128, 128, (P, H, 2, D)).astype(np.int8)
+        self.ref = Q.Cache.of(k, v, ks, vs, b, table)
+        t = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+        self.dev = QuantCache(t(k).view(E4M3), t(v).view(E4M3), t(ks), t(vs), t(b), t(table))
+        self.lens = [0] * rows
+
+    def tokens(self, counts, heads, dtype, std=1.0, stride=None, shift=0):
+        """[n_tok, heads, D] values of the type as (device tensor, float64 array); stride: a wider row; shift:
+        elements that its first one lies off the allocation's start."""
+        import torch
+        n, w = sum(counts), heads * self.D
+        x = torch.from_numpy(self.rng.normal(size=(n, w)) * std).to(dtype_of(dtype))
+        ld = stride or w
+        buf = torch.zeros(max(n, 1) * ld + shift, dtype=x.dtype, device="cuda")
+        d = torch.as_strided(buf, (n, w), (ld, 1), shift)
+        d.copy_(x)
+        return d.unflatten(1, (heads, self.D)), x.double().numpy().reshape(n, heads, self.D)
+
+    def where(self, counts):
+        import torch
+        off = torch.tensor(np.cumsum([0] + list(counts)), dtype=torch.int32).cuda()
+        return off, torch.tensor(self.lens, dtype=torch.int32).cuda()
+
+    def append(self, counts, dtype="f16", std=1.0, edit=None, **kw):
+        (k, k64), (v, v64) = (self.tokens(counts, self.H, dtype, std, **kw) for _ in range(2))
+        if edit is not None:
+            edit(k, k64)
+            edit(v, v64, True)
+        self.lens = [a + b for a, b in zip(self.lens, counts)]
+        off, lens = self.where(counts)
+        self.dev.append(k, v, off, lens, max_new=max(max(counts), 1))
+        o = 0
+        for r, n in enumerate(counts):
+            Q.append(self.ref, r, self.lens[r] - n, k64[o:o + n], v64[o:o + n])
+            o += n
+
+    def check(self):
+        import torch
+        d = self.dev
+        for name, got, want in (("k", d.k, self.ref.k), ("v", d.v, self.ref.v)):
+            a, b = got.view(torch.uint8).cpu().numpy(), want
+            nan = ((a & 127) == 127) & ((b & 127) == 127)
+            assert np.array_equal(np.where(nan, 0, a), np.where(nan, 0, b)), name
+        written = {self.ref.page(r, lp) for r in range(self.rows) for lp in range(-(-self.lens[r] // 64))} - {-1}
+        w = sorted(written)
+        assert np.array_equal(np.log2(d.k_scale.cpu().numpy()[w]), self.ref.ke[w])
+        assert np.array_equal(np.log2(d.v_scale.cpu().numpy()[w]), self.ref.ve[w])
+        assert np.array_equal(d.k_bounds.cpu().numpy().astype(int), self.ref.bounds)
+
+    def attend(self, counts, G, dtype="f16", n_select=0, scale=None, std=1.0, out_stride=None, max_len=None, **kw):
+        """Runs the attention, and holds every output to the reference."""
+        import torch
+        H, D, heads = self.H, self.D, self.H * G
+        scale = scale or 1 / math.sqrt(D)
+        q, q64 = self.tokens(counts, heads, dtype, std, **kw)
+        off, lens = self.where(counts)
+        out = None
+        if out_stride:
+            buf = torch.full((sum(counts), out_stride), 7.0, dtype=q.dtype, device="cuda")
+            out = buf[:, :heads * D].unflatten(1, (heads, D))
+        a = dict(max_new=max(max(counts), 1), max_len=max_len or max(max(self.lens), 1), scale=scale, out=out)
+        if n_select:
+            got, sel = self.dev.attend_selected(q, off, lens, n_select, **a)
+            sel = sel.cpu().numpy()
+        else:
+            got, sel = self.dev.attend(q, off, lens, **a), None
+        torch.cuda.synchronize()
+        if out_stride:
+            assert bool((buf[:, heads * D:] == 7.0).all())
+        self.compare(got.double().cpu().numpy(), sel, q64, counts, G, dtype, n_select, scale)
+        return got
+
+    def compare(self, got, sel, q64, counts, G, dtype, n_select, scale):
+        o = 0
+        for r, n in enumerate(counts):
+            for i in range(n):
+                vis = self.lens[r] - n + 1 + i
+                for h in range(self.H):
+                    qq = q64[o, h * G:(h + 1) * G]
+                    pages = None
+                    if n_select:
+                        pages = Q.select(self.ref, r, h, qq, vis, n_select)
+                        assert sel[o, h].tolist() == pages + [-1] * (n_select - len(pages)), (r, i, h)
+                    want, size, score = Q.attend(self.ref, r, h, qq, vis, scale, pages)
+                    x = got[o, h * G:(h + 1) * G]
+                    assert np.array_equal(np.isnan(x), np.isnan(want)), (r, i, h)
+                    # The output's rounding, and relative to sum p |v|: the rounding of the probabilities (fp16, or
+                    # a pair of them), a score's sum of 128 products and its exponent (each factor of exp once in the
+                    # numerator and once in the sum), the sums over the positions, two exponential instructions
+                    # (an ulp each).  Queries lose nothing but 2^-24 of a column's largest (one more product).
+                    p = 2.0 ** -22 if dtype == "f32" else 2.0 ** -11
+                    tol = HALF_STEP[dtype] * np.abs(want) + size * (
+                        p + 2 * score * (self.D + 8) * 2.0 ** -24 + 2 * max(vis, 1) * 2.0 ** -24 + 4 * 2.0 ** -23)
+                    assert np.all(np.nan_to_num(np.abs(x - want)) <= np.nan_to_num(tol) * (1 + HALF_STEP[dtype])), (
+                        r, i, h, float(np.nanmax(np.abs(x - want) - tol)))
+                o += 1
+
+
+# --- append ---------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("D,H", [(64, 1), (128, 3)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_append_in_pieces_writes_the_reference_bytes(D, H, dtype):
+    b = Both(3, 5, H, D, seed=D + H)
+    for counts, std in (((70, 1, 0), 1.0), ((1, 64, 129), 30.0), ((3, 5, 0), 0.01), ((58, 1, 1), 1000.0), ((0, 0, 66), 1e-9),
+                        ((4, 8, 9), 1.0), ((1, 1, 1), 5000.0)):
+        b.append(counts, dtype, std)
+        b.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [1, 2, 4, 5, 8, 9, 63, 64, 65, 66, 200])
+def test_append_at_every_offset_of_a_page(D, n):
+    b = Both(7, 8, 2, D, seed=n)
+    b.append((0, 1, 2, 3, 62, 63, 64), "f16", 0.3)
+    b.append((n,) * 7, "f16", 2.0)
+    b.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("stride,shift", [(0, 0), (5, 0), (8, 3), (1, 1)])
+def test_append_of_strided_and_unaligned_tokens(dtype, stride, shift):
+    b = Both(2, 3, 3, 128, seed=stride + shift)
+    b.append((67, 4), dtype, stride=3 * 128 + stride, shift=shift)
+    b.append((2, 3), dtype, stride=3 * 128 + stride, shift=shift)
+    b.check()
+
+
+def test_append_of_every_fp16_value():
+    """Each fp16 bit pattern once as a key and a value: saturation, subnormals, infinities, NaN."""
+    import torch
+    b = Both(8, 1, 8, 128, seed=1)
+    x = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.float16).view(64, 8, 128)
+
+    def edit(t, t64, value=False):
+        y = x.flip(0) if value else x
+        t.copy_(y)
+        t64[:] = y.double().numpy()
+    b.append((8,) * 8, "f16", edit=edit)
+    b.check()
+
+
+def test_append_skips_pages_outside_the_pool_and_negative_positions():
+    import torch
+    b = Both(3, 4, 2, 64, seed=5, table=[[3, -1, 2, 7], [1 << 30, 4, 5, 6], [-(1 << 31), 8, 9, 10]])
+    b.append((200, 130, 5), "f16")
+    b.check()
+    # 5 tokens of a row that is said to hold 3: the first two have no place
+    k, k64 = b.tokens((0, 5, 0), 2, "f16")
+    v, v64 = b.tokens((0, 5, 0), 2, "f16")
+    b.dev.page_table[1, 0] = 11
+    b.ref.table[1, 0] = 11
+    b.lens = [0, 3, 0]
+    off, lens = b.where((0, 5, 0))
+    b.dev.append(k, v, off, lens, max_new=5)
+    Q.append(b.ref, 1, -2, k64, v64)
+    b.lens = [0, 130, 0]
+    b.check()
+
+
+# --- attention ------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D,H,G", [(64, 2, 1), (128, 2, 1), (128, 1, 4), (64, 3, 7), (128, 1, 16), (64, 1, 20)])
+def test_decode_over_ragged_rows(dtype, D, H, G):
+    lens = (1, 2, 31, 32, 33, 64, 65, 130, 449)
+    b = Both(len(lens), 9, H, D, seed=D + G)
+    b.append(tuple(n - 1 for n in lens), "f16", 1.5)
+    b.append((1,) * len(lens), dtype, 1.5)
+    b.attend((1,) * len(lens), G, dtype, std=1.3)
+    b.attend((1, 0, 1, 0, 0, 1, 1, 0, 1), G, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("D,G,counts", [(128, 1, (9, 16, 0, 1, 5)), (64, 1, (17, 32, 3, 1, 20)), (128, 1, (33, 70, 1, 0, 65)),
+                                        (64, 4, (130, 40, 9, 1, 0)), (128, 1, (20, 32, 1, 0, 7)), (128, 3, (21, 43, 64, 2, 11)), (64, 20, (3, 1, 9, 2, 0))])
+def test_extension_and_build(dtype, D, G, counts):
+    b = Both(5, 6, 2, D, seed=sum(counts))
+    b.append((0, 1, 64, 127, 200), "bf16")
+    b.append(counts, dtype)
+    b.attend(counts, G, dtype)
+
+
+@pytest.mark.parametrize("D,G,dtype", [(128, 1, "f16"), (64, 8, "f32"), (128, 4, "bf16")])
+def test_long_row_in_many_splits(D, G, dtype):
+    b = Both(1, 80, 1, D, seed=G)
+    b.append((80 * 64 - 3,), "f16")
+    b.append((2,), "f16", 3.0)
+    b.attend((1,), G, dtype)
+    b.attend((2,), G, dtype, max_len=70)  # a wrong estimate of the length changes the split only
+    b.attend((40,), G, dtype)
+    b.attend((130,), 1, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("stride,shift", [(5, 0), (8, 3), (1, 1)])
+def test_strided_and_unaligned_queries_and_outputs(dtype, stride, shift):
+    b = Both(2, 3, 2, 64, seed=shift)
+    b.append((97, 70), "f16")
+    for counts in ((1, 1), (40, 33)):
+        b.attend(counts, 3, dtype, stride=6 * 64 + stride, shift=shift, out_stride=6 * 64 + stride + 2)
+
+
+@pytest.mark.parametrize("scale,std", [(1e-20, 1.0), (1.0, 1e-6), (30.0, 1.0), (0.1, 2000.0)])
+def test_scores_from_nothing_to_one_position_taking_all(scale, std):
+    b = Both(2, 3, 1, 128, seed=3)
+    b.append((100, 64), "f16")
+    b.attend((1, 3), 2, "f32", scale=scale, std=std)
+    b.attend((1, 3), 2, "f16", scale=scale, std=std)
+
+
+def test_pages_of_very_different_scales():
+    b = Both(1, 8, 1, 64, seed=11)
+    for std in (1e-8, 1.0, 3000.0, 1e-3, 50.0, 1e-9, 1.0):
+        b.append((64,), "f32", std)
+    b.append((10,), "f32", 2.0)
+    for counts in ((1,), (40,)):
+        b.attend(counts, 1, "f32", std=1e-2)
+        b.attend(counts, 2, "f16", std=1e-2)
+
+
+def test_rows_that_see_nothing_are_zero_and_foreign_tokens_keep_theirs():
+    import torch
+    b = Both(3, 2, 2, 64, seed=9, table=[[0, 1], [-1, 5], [2, 99]])
+    b.append((20, 100, 0), "f16")
+    # row 0: more new tokens than positions; row 1: its first page lies outside the pool; row 2 holds nothing
+    b.lens = [2, 100, 0]
+    b.attend((5, 60, 3), 2, "f16")
+    b.lens = [20, 100, 0]
+    q, _ = b.tokens((5, 60, 3), 4, "f16")
+    out = torch.full_like(q, 3.0)
+    off = torch.tensor([4, 5, 5, 6], dtype=torch.int32).cuda()  # tokens 0..3 and 6.. belong to nobody
+    b.dev.attend(q, off, torch.tensor(b.lens, dtype=torch.int32).cuda(), out=out)
+    torch.cuda.synchronize()
+    assert bool((out[:4] == 3).all()) and bool((out[6:] == 3).all())
+    assert not bool((out[4:5] == 3).any()) and bool((out[5] == 0).all())
+
+
+def test_nan_and_infinities_reach_only_those_who_see_them():
+    b = Both(1, 3, 2, 64, seed=13)
+
+    def edit(t, t64, value=False):
+        for tok, head, ch, x in ((30, 0, 5, float("nan")), (10, 1, 2, float("inf")), (60, 1, 0, float("-inf"))):
+            if value == (tok == 30):
+                t[tok, head, ch] = x
+                t64[tok, head, ch] = x
+    b.append((90,), "f32", edit=edit)
+    b.check()
+    for n in (1, 8, 90):
+        b.attend((n,), 1, "f16")
+    b.attend((90,), 4, "f32")
+
+
+# --- selection ------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D,H,G,n_select", [(64, 2, 1, 4), (128, 1, 4, 3), (128, 2, 2, 1), (64, 1, 20, 5), (64, 1, 8, 40)])
+def test_selected_pages_and_their_attention(dtype, D, H, G, n_select):
+    b = Both(4, 30, H, D, seed=n_select)
+    for std in (1.0, 4.0, 0.2):
+        b.append((5, 64, 300, 601), "f16", std)
+    for counts in ((1, 1, 1, 1), (3, 0, 2, 5)):
+        b.append(counts, dtype)
+        b.attend(counts, G, dtype, n_select=n_select)
+
+
+def test_selection_over_many_pages():
+    b = Both(1, 1100, 1, 64, seed=21)
+    for _ in range(11):
+        b.append((6400 - 50,), "f16", float(np.exp(b.rng.normal())))
+    b.attend((1,), 4, "f16", n_select=64)
+    b.attend((2,), 1, "f16", n_select=300)
+
+
+def test_selection_ties_and_missing_pages():
+    import torch
+    table = np.arange(40, dtype=np.int32)[None].copy()
+    table[0, [3, 17, 39]] = (-1, 77, 1000)
+    b = Both(1, 40, 1, 64, seed=22, table=table, spare=0)
+    b.append((40 * 64,), "f16")
+    same = b.ref.bounds[5].copy()
+    b.ref.bounds[:] = same  # every page promises the same: the lowest pages are chosen
+    b.dev.k_bounds.copy_(torch.from_numpy(np.broadcast_to(same, b.ref.bounds.shape).astype(np.int8)))
+    b.ref.ke[:] = -7
+    b.dev.k_scale.fill_(2.0 ** -7)
+    for n in (1, 2, 8, 36, 37, 38, 39, 40, 64):
+        b.attend((1,), 2, "f16", n_select=n)
+    b.attend((3,), 2, "f32", n_select=9, std=0.0)
+
+
+# --- together -------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("n_select", [0, 3])
+def test_a_decode_loop_in_a_graph_follows_its_lengths(n_select):
+    """Append and attention of one token per row captured once, replayed while the rows grow (across page
+    ends), with eager work of other caches between the replays."""
+    import torch
+    rows, H, G, D = 4, 2, 2, 64
+    b = Both(rows, 6, H, D, seed=31)
+    b.append((61, 5, 190, 254), "f16")
+    k, v = (torch.empty(rows, H, D, dtype=torch.float16, device="cuda") for _ in range(2))
+    q = torch.empty(rows, H * G, D, dtype=torch.float16, device="cuda")
+    off = torch.arange(rows + 1, dtype=torch.int32, device="cuda")
+    lens = torch.tensor(b.lens, dtype=torch.int32, device="cuda")
+
+    def step():
+        b.dev.append(k, v, off, lens, max_new=1)
+        if n_select:
+            return b.dev.attend_selected(q, off, lens, n_select, max_new=1, max_len=384)
+        return b.dev.attend(q, off, lens, max_new=1, max_len=384), None
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        kept = [t.clone() for t in (b.dev.k.view(torch.uint8), b.dev.v.view(torch.uint8), b.dev.k_scale, b.dev.v_scale, b.dev.k_bounds)]
+        for t in (k, v, q):
+            t.zero_()
+        step()
+        for t, x in zip((b.dev.k.view(torch.uint8), b.dev.v.view(torch.uint8), b.dev.k_scale, b.dev.v_scale, b.dev.k_bounds), kept):
+            t.copy_(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, sel = step()
+    for r in range(6):
+        (kn, k64), (vn, v64), (qn, q64) = (b.tokens((1,) * rows, n, "f16") for n in (H, H, H * G))
+        for t, x in ((k, kn), (v, vn), (q, qn)):
+            t.copy_(x)
+        b.lens = [n + 1 for n in b.lens]
+        lens.copy_(torch.tensor(b.lens, dtype=torch.int32))
+        for i in range(rows):
+            Q.append(b.ref, i, b.lens[i] - 1, k64[i:i + 1], v64[i:i + 1])
+        graph.replay()
+        torch.cuda.synchronize()
+        b.check()
+        b.compare(out.double().cpu().numpy(), None if sel is None else sel.cpu().numpy(), q64, (1,) * rows, G, "f16",
+                  n_select, 1 / math.sqrt(D))
+        other = Both(2, 2, H, D, seed=100 + r)
+        other.append((70, 3), "f16")
+        other.attend((1, 2), G, "f16", n_select=n_select)
+
+
+def test_two_streams_and_repeated_calls_give_the_same_bits():
+    import torch
+    b = Both(2, 40, 2, 128, seed=41)
+    b.append((2000, 900), "f16")
+    q, _ = b.tokens((1, 1), 8, "bf16")
+    off, lens = b.where((1, 1))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = []
+    for r in range(6):
+        with torch.cuda.stream(streams[r % 2]):
+            outs.append(b.dev.attend(q, off, lens, max_new=1, max_len=2000))
+            outs.append(b.dev.attend_selected(q, off, lens, 5, max_new=1, max_len=2000)[0])
+    torch.cuda.synchronize()
+    for a in outs[2::2]:
+        assert torch.equal(a, outs[0])
+    for a in outs[3::2]:
+        assert torch.equal(a, outs[1])
+
+
+def test_results_do_not_depend_on_other_rows():
+    """A row's outputs have the same bits alone and in a batch whose launch is split alike."""
+    import torch
+    b = Both(3, 4, 2, 64, seed=43)
+    b.append((200, 100, 37), "f16")
+    q, _ = b.tokens((20, 20, 20), 4, "f16")
+    off, lens = b.where((20, 20, 20))
+    one = b.dev.attend(q, off, lens, max_new=20, max_len=200)
+    alone = torch.tensor([0, 0, 20, 20], dtype=torch.int32).cuda()
+    two = b.dev.attend(q[20:40], alone, lens, max_new=20, max_len=200)
+    torch.cuda.synchronize()
+    assert torch.equal(one[20:40], two)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows at the end of a pool of more than 2^32 bytes."""
+    import torch
+    from paper_2508_10259_amd.qcache import QuantCache
+    H, D, P = 8, 128, 70000  # 4.6e9 bytes of keys
+    table = torch.tensor([[P - 1, P - 2, 1], [P - 3, 0, P - 4]], dtype=torch.int32, device="cuda")
+    big = QuantCache.empty(P, H, D, table)
+    small = QuantCache.empty(6, H, D, torch.tensor([[0, 1, 2], [3, 4, 5]], dtype=torch.int32, device="cuda"))
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k, v, q = (torch.randn(300, H, D, device="cuda", generator=g).half() for _ in range(3))
+    off = torch.tensor([0, 170, 300], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([170, 130], dtype=torch.int32, device="cuda")
+    outs = []
+    for c in (big, small):
+        c.append(k, v, off, lens, max_new=170)
+        outs.append(c.attend(q, off, lens, max_new=170))
+        outs.append(c.attend_selected(q, off, lens, 2, max_new=170)[0])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
+    del big
+    torch.cuda.empty_cache()

@@ -1,0 +1,105 @@
+"""Refusals of the 8-bit cache calls: made before anything is looked up on a device, so they run here."""
+import ctypes as C
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2508_10259_amd import capi
+    return capi.load()
+
+
+def _cache(**kw):
+    from paper_2508_10259_amd.capi import QCache
+    base = dict(k=4096, v=4096, k_scale=4096, v_scale=4096, k_bounds=4096, page_table=4096, n_pages=8, n_kv_heads=2,
+                head_dim=64, rows=2, pages_per_row=4)
+    base.update(kw)
+    return QCache(**base)
+
+
+BAD_DIMS = [dict(head_dim=96), dict(head_dim=0), dict(n_kv_heads=0), dict(n_kv_heads=1025), dict(n_pages=0),
+            dict(n_pages=(1 << 28) + 1), dict(rows=0), dict(rows=65536), dict(pages_per_row=0), dict(pages_per_row=16385)]
+
+
+def _append(lib, c, n_tok=4, max_new=2, ldk=128, ldv=128, dtype=2, **kw):
+    return lib.ams_qcache_append(C.byref(c) if c is not None else None, 64, 64, n_tok, max_new, 4096, ldk, 4096, ldv, dtype, None)
+
+
+def _attend(lib, c, n_tok=4, max_new=2, max_len=100, n_heads=4, ldq=256, ldo=256, dtype=2, scale=0.1, n_select=0,
+            selected=None, ws=4096, ws_bytes=1 << 30):
+    return lib.ams_qcache_attend(C.byref(c) if c is not None else None, 64, 64, n_tok, max_new, max_len, n_heads, 4096, ldq,
+                                 4096, ldo, dtype, scale, n_select, selected, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("bad", BAD_DIMS)
+def test_dimensions(lib, bad):
+    c = _cache(**bad)
+    assert _append(lib, c) == -1 and _attend(lib, c) == -1 and lib.ams_last_error()
+    assert lib.ams_qcache_workspace_bytes(C.byref(c), 4, 4, 2, 100, 0) == 0
+
+
+def test_null_cache(lib):
+    assert _append(lib, None) == -1 and _attend(lib, None) == -1
+    assert lib.ams_qcache_workspace_bytes(None, 4, 4, 2, 100, 0) == 0
+
+
+@pytest.mark.parametrize("bad", [dict(n_tok=-1), dict(max_new=0), dict(dtype=3), dict(dtype=-1)])
+def test_append_arguments(lib, bad):
+    assert _append(lib, _cache(), **bad) == -1
+
+
+@pytest.mark.parametrize("bad", [dict(n_tok=-1), dict(max_new=0), dict(max_len=0), dict(n_heads=3), dict(n_heads=0),
+                                 dict(dtype=5), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+                                 dict(scale=float("inf")), dict(n_select=-1), dict(n_select=16385),
+                                 dict(selected=64), dict(ws=None), dict(ws=4104), dict(n_select=2, selected=66)])
+def test_attend_arguments(lib, bad):
+    assert _attend(lib, _cache(), **bad) == -1
+
+
+def test_attend_workspace_too_small(lib):
+    assert _attend(lib, _cache(), n_select=2, ws_bytes=8) == -6
+
+
+def test_no_tokens_is_no_call(lib):
+    assert _append(lib, _cache(), n_tok=0) == 0 and _attend(lib, _cache(), n_tok=0) == 0
+    assert lib.ams_qcache_workspace_bytes(C.byref(_cache()), 4, 0, 2, 100, 0) >= 1
+
+
+def test_too_large_a_launch(lib):
+    c = _cache(rows=65535, n_kv_heads=1024)
+    assert _append(lib, c, n_tok=1 << 30, max_new=1 << 20) == -1
+    assert _attend(lib, c, n_tok=1 << 30, max_new=1 << 20, n_heads=1024) == -1
+
+
+def test_workspace_grows_with_splits_and_lists(lib):
+    c = _cache(rows=1, pages_per_row=4096)
+    one = lib.ams_qcache_workspace_bytes(C.byref(c), 4, 1, 1, 64, 0)
+    long = lib.ams_qcache_workspace_bytes(C.byref(c), 4, 1, 1, 1 << 18, 0)
+    listed = lib.ams_qcache_workspace_bytes(C.byref(c), 4, 1, 1, 64, 8)
+    assert 1 <= one < long and listed >= one + 2 * 8 * 4
+
+
+def test_python_checks():
+    import torch
+    from paper_2508_10259_amd.qcache import QuantCache
+    c = QuantCache.empty(4, 2, 64, torch.zeros(1, 2, dtype=torch.int32))
+    off, lens = torch.tensor([0, 3], dtype=torch.int32), torch.tensor([3], dtype=torch.int32)
+    x = torch.zeros(3, 2, 64)
+    for bad in (dict(k=x[:, :1]), dict(k=x.double()), dict(k=x.transpose(1, 2)), dict(tok_off=off[:1]), dict(tok_off=off.long()),
+                dict(lens=torch.zeros(2, dtype=torch.int32)), dict(v=x.half())):
+        a = dict(k=x, v=x, tok_off=off, lens=lens)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            c.append(**a)
+    for bad in (dict(q=x.transpose(0, 1)), dict(out=x.half()), dict(out=x[:2])):
+        a = dict(q=x, tok_off=off, lens=lens)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            c.attend(**a)
+    with pytest.raises(ValueError):
+        c.attend_selected(x, off, lens, 0)
+    with pytest.raises(ValueError):
+        c.attend_selected(x, off, lens, 2, selected=torch.zeros(3, 2, 3, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        QuantCache(c.k, c.v, c.k_scale, c.v_scale[:2], c.k_bounds, c.page_table)
