@@ -312,9 +312,20 @@ void ams_ctx_destroy(ams_ctx* c); /* NULL is a no-op */
  * context's up to rounding (shared pages may come from a pass of other rows). */
 #define AMS_CTX_SHARE_PREFIX 1
 
+/* A context whose K/V are held in 8 bits, an ams_qcache per layer: half the K/V
+ * memory of an fp16 context (a quarter of an fp32 one), and host images of rows
+ * that are as much smaller.  Builds, appends, steps and flow append to it and
+ * attend over it (a row's own new tokens too, so a step gives what a rebuilt
+ * context gives but for the codes that a growing scale rounded again); the action
+ * decode runs as per-layer kernels.  Keys and values carry 4 significant bits:
+ * logits differ from an fp16 context's by that much.  Scratch positions that a step
+ * drops can leave a page's scale and bounds larger than its committed positions
+ * need.  See ams_qcache_append and ams_ctx_select_pages. */
+#define AMS_CTX_QCACHE 2
+
 /* Bytes of workspace of a paged context: as ams_ctx_workspace_bytes with
- * n_pages K/V pages per layer pool (0: batch * capacity / 64) and `flags`
- * (0 or AMS_CTX_SHARE_PREFIX).  0 if an argument is invalid. */
+ * n_pages K/V pages per layer pool (0: batch * capacity / 64) and `flags` (any
+ * of AMS_CTX_SHARE_PREFIX and AMS_CTX_QCACHE).  0 if an argument is invalid. */
 size_t ams_ctx_workspace_bytes_paged(const ams_model_cfg* cfg, int32_t batch, int32_t capacity,
                                      int32_t max_pass_tokens, int32_t n_pages, int32_t flags);
 
@@ -419,7 +430,10 @@ ams_status ams_ctx_append(ams_ctx* c, const void* new_tokens, const int32_t* new
  * [1, capacity]): a 256-byte header, every layer's K and V of the row's
  * positions ([layer][K|V][head][len][head_dim] in the compute type: fp16 for
  * bf16 models, fp32 otherwise), the last position's hidden state (fp32 [d])
- * and its fp16 pair ([d] + [d]). */
+ * and its fp16 pair ([d] + [d]).  An AMS_CTX_QCACHE context's image holds whole
+ * pages instead: per layer, page and head the key codes, the value codes, the
+ * bounds and the two scales (16 bytes with padding), in ams_qcache's layouts
+ * (positions behind the row's last hold anything). */
 size_t ams_ctx_row_host_bytes(const ams_ctx* c, int32_t len);
 
 /* Copies each listed row's context (READY rows; strictly increasing indices)
@@ -442,6 +456,15 @@ ams_status ams_ctx_offload_rows(ams_ctx* c, const int32_t* rows, int32_t n_rows,
  * nothing changed), AMS_EHIP. */
 ams_status ams_ctx_reload_rows(ams_ctx* c, const int32_t* rows, int32_t n_rows, const void* const* host,
                                void* stream);
+
+/* How many pages of 64 positions each query of the action decode attends to in
+ * every layer and head of an AMS_CTX_QCACHE context: the page of its own position
+ * and the n_pages - 1 others whose keys' bounds promise the largest scores
+ * (n_select of ams_qcache_attend).  0, as after creation, or the row capacity's
+ * pages and more: all of them.  Prefixes and new observation tokens are always
+ * computed over everything.  Applies to the steps enqueued after the call.
+ * Errors: AMS_EINVAL (no such context, n_pages < 0). */
+ams_status ams_ctx_select_pages(ams_ctx* c, int32_t n_pages);
 
 /* Each row's state into host array states[batch]: 0 EMPTY, 1 READY,
  * 2 INVALID, 3 OFFLOADED. */

@@ -12,7 +12,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libams.so")
 
 AMS_OK, AMS_EINVAL, AMS_ESTATE, AMS_ECAPACITY, AMS_ENODEV, AMS_EHIP, AMS_ENOMEM = 0, -1, -2, -3, -4, -5, -6
 AMS_F32, AMS_BF16, AMS_F16 = 0, 1, 2
-AMS_CTX_SHARE_PREFIX = 1
+AMS_CTX_SHARE_PREFIX, AMS_CTX_QCACHE = 1, 2
 STATE_EMPTY, STATE_READY, STATE_INVALID, STATE_OFFLOADED = 0, 1, 2, 3
 
 
@@ -79,6 +79,7 @@ SIGNATURES = {
                                          C.c_void_p]),
     "ams_ctx_reload_rows": (C.c_int32, [C.c_void_p, C.POINTER(C.c_int32), C.c_int32, C.POINTER(C.c_void_p),
                                         C.c_void_p]),
+    "ams_ctx_select_pages": (C.c_int32, [C.c_void_p, C.c_int32]),
     "ams_ctx_row_states": (C.c_int32, [C.c_void_p, C.POINTER(C.c_int32)]),
     "ams_ctx_flow": (C.c_int32, [C.c_void_p, C.POINTER(FlowHead), C.c_void_p, C.c_float, C.c_int32, C.c_void_p]),
     "ams_tier_plan": (C.c_int32, [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,

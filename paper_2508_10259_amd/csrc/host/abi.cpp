@@ -206,7 +206,7 @@ size_t ams_ctx_workspace_bytes(const ams_model_cfg* cfg, int32_t batch, int32_t 
 }
 
 static int check_paged(int batch, int capacity, int32_t n_pages, int32_t flags, std::string& e) {
-  if (flags & ~AMS_CTX_SHARE_PREFIX) {
+  if (flags & ~(AMS_CTX_SHARE_PREFIX | AMS_CTX_QCACHE)) {
     e = "unknown context flags";
     return AMS_EINVAL;
   }
@@ -225,7 +225,9 @@ size_t ams_ctx_workspace_bytes_paged(const ams_model_cfg* cfg, int32_t batch, in
   if (ams::check_cfg(c, e) != ams::S_OK) return 0;
   if (ams::check_ctx_args(c, batch, capacity, max_pass_tokens, e) != ams::S_OK) return 0;
   if (check_paged(batch, capacity, n_pages, flags, e) != AMS_OK) return 0;
-  return ams::ctx_layout(c, batch, capacity, max_pass_tokens, n_pages, flags & AMS_CTX_SHARE_PREFIX).total;
+  return ams::ctx_layout(c, batch, capacity, max_pass_tokens, n_pages, flags & AMS_CTX_SHARE_PREFIX,
+                         flags & AMS_CTX_QCACHE)
+      .total;
 }
 
 static ams_status ctx_create(ams_model* m, int32_t batch, int32_t capacity, int32_t max_pass_tokens,
@@ -236,7 +238,8 @@ static ams_status ctx_create(ams_model* m, int32_t batch, int32_t capacity, int3
   if (int s = ams::check_ctx_args(m->m.cfg, batch, capacity, max_pass_tokens, e)) return fail(s, e);
   if (int s = check_paged(batch, capacity, n_pages, flags, e)) return fail(s, e);
   const ams::CtxLayout lay =
-      ams::ctx_layout(m->m.cfg, batch, capacity, max_pass_tokens, n_pages, flags & AMS_CTX_SHARE_PREFIX);
+      ams::ctx_layout(m->m.cfg, batch, capacity, max_pass_tokens, n_pages, flags & AMS_CTX_SHARE_PREFIX,
+                      flags & AMS_CTX_QCACHE);
   if (!ws) return fail(AMS_EINVAL, "workspace is NULL");
   if (!aligned256(ws)) return fail(AMS_EINVAL, "workspace must be 256-byte aligned");
   if (ws_bytes < lay.total) return fail(AMS_ENOMEM, "context workspace too small: need " + std::to_string(lay.total));
@@ -626,6 +629,8 @@ ams_status ams_qcache_attend(const ams_qcache* cache, const int32_t* tok_off, co
 
 namespace {
 constexpr uint32_t ROW_IMAGE_MAGIC = 0x52534D41u;  // "AMSR"
+constexpr uint32_t ROW_IMAGE_VERSION = 1u, ROW_IMAGE_QCACHE = 2u;  // the latter: 8-bit pages
+uint32_t image_version(const ams::Ctx& x) { return x.lay.qcache ? ROW_IMAGE_QCACHE : ROW_IMAGE_VERSION; }
 struct RowImageHeader {
   uint32_t magic, version;
   int32_t len, n_layers, d_model, head_dim, n_heads, dtype;
@@ -650,7 +655,8 @@ bool host_device_ptr(const void* p, void** dev, std::string& err) {
 
 size_t ams_ctx_row_host_bytes(const ams_ctx* c, int32_t len) {
   if (!c || len < 1 || len > c->c.lay.capacity) return 0;
-  return ams::row_host_bytes(c->c.model->cfg, len);
+  return c->c.lay.qcache ? ams::row_host_bytes_qcache(c->c.model->cfg, len)
+                         : ams::row_host_bytes(c->c.model->cfg, len);
 }
 
 ams_status ams_ctx_offload_rows(ams_ctx* c, const int32_t* rows, int32_t n_rows, void* const* host, void* stream) {
@@ -670,7 +676,7 @@ ams_status ams_ctx_offload_rows(ams_ctx* c, const int32_t* rows, int32_t n_rows,
   }
   const ams::Cfg& m = x.model->cfg;
   for (int i = 0; i < n_rows; ++i) {
-    RowImageHeader hd{ROW_IMAGE_MAGIC, 1u, lens[i], m.n_layers, m.d_model, m.head_dim, m.n_heads, m.dtype};
+    RowImageHeader hd{ROW_IMAGE_MAGIC, image_version(x), lens[i], m.n_layers, m.d_model, m.head_dim, m.n_heads, m.dtype};
     memcpy(host[i], &hd, sizeof(hd));
   }
   if (int s = ams::ctx_offload_rows(x, rows, n_rows, lens.data(), dev.data(), (hipStream_t)stream, e)) {
@@ -698,7 +704,7 @@ ams_status ams_ctx_reload_rows(ams_ctx* c, const int32_t* rows, int32_t n_rows, 
     if (((uintptr_t)host[i] & 15) != 0) return fail(AMS_EINVAL, "host buffers must be 16-byte aligned");
     RowImageHeader hd;
     memcpy(&hd, host[i], sizeof(hd));
-    if (hd.magic != ROW_IMAGE_MAGIC || hd.version != 1u || hd.n_layers != m.n_layers || hd.d_model != m.d_model ||
+    if (hd.magic != ROW_IMAGE_MAGIC || hd.version != image_version(x) || hd.n_layers != m.n_layers || hd.d_model != m.d_model ||
         hd.head_dim != m.head_dim || hd.n_heads != m.n_heads || hd.dtype != m.dtype)
       return fail(AMS_EINVAL, "host buffer " + std::to_string(i) + " holds no row image of this model");
     if (hd.len < 1 || hd.len > x.lay.capacity)
@@ -710,6 +716,16 @@ ams_status ams_ctx_reload_rows(ams_ctx* c, const int32_t* rows, int32_t n_rows, 
     return fail(s, e);
   }
   x.book.commit_build_rows(rows, n_rows, lens.data());
+  return AMS_OK;
+}
+
+ams_status ams_ctx_select_pages(ams_ctx* c, int32_t n_pages) {
+  g_err.clear();
+  if (!c) return fail(AMS_EINVAL, "context is NULL");
+  if (!c->c.lay.qcache) return fail(AMS_EINVAL, "only a context with AMS_CTX_QCACHE selects pages");
+  if (n_pages < 0) return fail(AMS_EINVAL, "n_pages must be >= 0");
+  // a row never has more pages than its capacity: selecting that many is attending to all
+  c->c.select = n_pages >= c->c.lay.ppr ? 0 : n_pages;
   return AMS_OK;
 }
 

@@ -3,6 +3,7 @@
 // captured once per (n_actions, output buffers) into a HIP graph and replayed.
 #include "engine.h"
 
+#include <math.h>
 #include <stdlib.h>
 
 #include "../kernels/kernels.h"
@@ -92,7 +93,7 @@ static bool fused_applies(const Ctx& c) {
   if (e && e[0] == '0') return false;
   const Cfg& m = c.model->cfg;
   const int B = c.lay.batch;
-  if (c.model->ct != DT_F16 || B > FUSED_MAX_ROWS) return false;
+  if (c.model->ct != DT_F16 || B > FUSED_MAX_ROWS || c.lay.qcache) return false;
   if (m.head_dim != 64 && m.head_dim != 128) return false;
   if (m.d_model % 128 != 0 || m.d_ffn % 128 != 0 || bins_padded(m) % 16 != 0) return false;
   return c.lay.slab_layer < ((size_t)1 << 31) && (size_t)B * 3 * m.d_model * 4 < ((size_t)1 << 31) &&
@@ -261,10 +262,15 @@ static int rows_xfer_enqueue(Ctx& c, bool to_host, const int32_t* rows, int n_ro
   c.xfer_host.resize(n_rows);
   for (int i = 0; i < n_rows; ++i) c.xfer_host[i] = XferRow{rows[i], lens[i], host_dev[i]};
   XferRow* xd = (XferRow*)(c.ws + c.lay.xfer);
-  if (hipMemcpyAsync(xd, c.xfer_host.data(), n_rows * sizeof(XferRow), hipMemcpyHostToDevice, s) != hipSuccess ||
-      rows_xfer(to_host, xd, n_rows, m.n_layers, m.n_heads, m.head_dim, (int)(c.model->ct == DT_F16 ? 2 : 4),
-                c.ws + c.lay.kv, c.lay.slab_layer, c.pt(), c.lay.ppr, c.h_last(), c.h_last16(), c.h_last16lo(),
-                m.d_model, s) != hipSuccess) {
+  hipError_t e = hipMemcpyAsync(xd, c.xfer_host.data(), n_rows * sizeof(XferRow), hipMemcpyHostToDevice, s);
+  if (e == hipSuccess && c.lay.qcache)
+    e = rows_xfer_qcache(to_host, xd, n_rows, m.n_layers, c.qcache(0, 0, c.lay.batch), 2 * c.lay.slab_layer,
+                         c.lay.scale_layer, c.lay.bound_layer, c.h_last(), c.h_last16(), c.h_last16lo(), m.d_model, s);
+  else if (e == hipSuccess)
+    e = rows_xfer(to_host, xd, n_rows, m.n_layers, m.n_heads, m.head_dim, (int)(c.model->ct == DT_F16 ? 2 : 4),
+                  c.ws + c.lay.kv, c.lay.slab_layer, c.pt(), c.lay.ppr, c.h_last(), c.h_last16(), c.h_last16lo(),
+                  m.d_model, s);
+  if (e != hipSuccess) {
     err = to_host ? "offload to host memory failed" : "reload from host memory failed";
     return S_EHIP;
   }
@@ -318,7 +324,7 @@ int ctx_absorb_status(Ctx& c, std::string& err) {
 // columns of qkv saved).
 static bool kv_fusable(const Ctx& c, int M) {
   const Cfg& m = c.model->cfg;
-  return c.model->ct == DT_F16 && gemm_qkv_fusable(M, 3 * m.d_model, m.head_dim, m.d_model);
+  return c.model->ct == DT_F16 && !c.lay.qcache && gemm_qkv_fusable(M, 3 * m.d_model, m.head_dim, m.d_model);
 }
 
 // h += x W^T over the M tokens of a token pass (K inputs per token; Wf: W in
@@ -370,6 +376,24 @@ static hipError_t tokens_proj(const Ctx& c, int epi, const void* W, const void* 
   return part_store(c.kpart(), S, M, N, (float*)out, s);
 }
 
+// 8-bit K/V: the append and the attention of layer l over the tokens of `sg`, whose projections lie in qkv
+// (fp32 [token][3d], keys and queries rotated on the way); select > 0: over that many pages of each query.
+// An fp32 model's output is fp32; an fp16 one's rounding errors go to olo when given, and pair asks
+// for fp16 pairs inside (its decode passes; token passes round queries once, as their other inputs).
+static hipError_t attn_qcache(const Ctx& c, const QCache& qc, const QSegs& sg, int max_end, int select, const float* qkv,
+                              bool pair, void* o, void* olo, hipStream_t s) {
+  const Cfg& m = c.model->cfg;
+  const int d = m.d_model, H = m.n_heads, dh = m.head_dim, ct = c.model->ct;
+  hipError_t e = qcache_append(qc, sg, qkv + d, 3 * d, qkv + 2 * d, 3 * d, DT_F32, c.rope(), s);
+  int32_t* sel = select > 0 ? (int32_t*)(c.ws + c.lay.qc_sel) : nullptr;
+  if (e == hipSuccess && sel) e = qcache_select(qc, sg, H, qkv, 3 * d, DT_F32, c.rope(), select, sel, s);
+  if (e != hipSuccess) return e;
+  const QAttendPlan p =
+      qcache_attend_plan(sg.n_seg, H, H, dh, sg.n_tok, sg.max_new, max_end, select, c.lay.qc_part_floats);
+  return qcache_attend(qc, sg, p, H, qkv, 3 * d, DT_F32, pair || ct == DT_F32, 1.0f / sqrtf((float)dh), c.rope(), sel,
+                       select, o, d, ct, olo, (float*)(c.ws + c.lay.qc_part), s);
+}
+
 // One decoder layer over the M tokens of a token pass; u_ready: u already holds
 // RMSNorm(h) (left by the previous residual reduction), and on return whether
 // it holds the norm of this layer's output; tables: the pass's token tables
@@ -388,14 +412,17 @@ static hipError_t layer_tokens(Ctx& c, int l, int M, const Segs& sg, hipStream_t
     TRY(gemm_qkv_kv(c.u(), md.fqkv(l), M, d, c.qkv(), kv, s));
   } else {
     TRY(tokens_proj(c, EPI_STORE, md.wqkv(l), md.fqkv(l), M, 3 * d, d, c.qkv(), 3 * d, s));
-    if (tables)  // each token's slot from the pass's tables (7B batch-64 extension: 19.05 -> 18.92 ms per step)
+    if (c.lay.qcache)
+      TRY(attn_qcache(c, c.qcache(l, 0, c.lay.batch), QSegs{sg.row, sg.off, sg.pos, nullptr, 0, sg.n_seg, M, sg.max_len},
+                      sg.max_end, 0, c.qkv(), false, c.o(), nullptr, s));
+    else if (tables)  // each token's slot from the pass's tables (7B batch-64 extension: 19.05 -> 18.92 ms per step)
       TRY(kv_append_tab(c.qkv(), M, (const int64_t*)(c.ws + c.lay.tok_base), (const int32_t*)(c.ws + c.lay.tok_pos),
                         m.n_heads, m.head_dim, c.rope(), c.kslab(l), c.vslab(l), s));
     else
       TRY(kv_append(dt, c.qkv(), sg, m.n_heads, m.head_dim, c.pages(), c.rope(), c.kslab(l), c.vslab(l), s));
   }
-  TRY(attn_prefill(dt, c.qkv(), sg, m.n_heads, m.head_dim, c.pages(), c.rope(), c.kslab(l), c.vslab(l), c.o(),
-                   s));
+  if (!c.lay.qcache)
+    TRY(attn_prefill(dt, c.qkv(), sg, m.n_heads, m.head_dim, c.pages(), c.rope(), c.kslab(l), c.vslab(l), c.o(), s));
   TRY(tokens_resid(c, c.o(), md.wo(l), md.fo(l), M, d, s, u_ready));
   if (!u_ready && !f32s) TRY(rmsnorm(dt, c.h(), M, d, m.rms_eps, c.u(), s));
   TRY(tokens_proj(c, EPI_SWIGLU, md.wgu(l), md.fgu(l), M, 2 * F, d, c.a(), F, s));
@@ -431,7 +458,7 @@ hipError_t ctx_forward_tokens(Ctx& c, const void* x, const int32_t* counts, cons
     else
       TRY(ingest(c.model->st, (const char*)x + (size_t)ps.tok_src * d * es, ps.n_tok, (int)d, c.h(), s));
     bool u_ready = false;
-    const bool tabs = c.model->ct == DT_F16, kvf = kv_fusable(c, ps.n_tok);
+    const bool tabs = c.model->ct == DT_F16 && !c.lay.qcache, kvf = kv_fusable(c, ps.n_tok);
     if (tabs)
       TRY(tok_tables(sg, c.pages(), m.n_heads, m.head_dim, (int64_t*)(c.ws + c.lay.tok_base),
                      (int32_t*)(c.ws + c.lay.tok_pos), s));
@@ -469,7 +496,7 @@ hipError_t ctx_flow(Ctx& c, const FlowHeadView& fh, float* x, float tau0, int n_
               ps.max_len, ps.max_end, md + 6 * B + 1 + ps.seg_begin};
       float* xp = x + (size_t)ps.tok_src * a;  // every row brings T tokens: the pass's first token
       TRY(flow_embed(c.model->st, xp, fh.w_in, fh.w_t, tau, ps.n_tok, a, d, c.h(), s));
-      const bool tabs = c.model->ct == DT_F16;
+      const bool tabs = c.model->ct == DT_F16 && !c.lay.qcache;
       if (tabs)
         TRY(tok_tables(sg, c.pages(), m.n_heads, m.head_dim, (int64_t*)(c.ws + c.lay.tok_base),
                        (int32_t*)(c.ws + c.lay.tok_pos), s));
@@ -611,11 +638,16 @@ static hipError_t layer_decode(const Rows& g, int l, int jpos, hipStream_t s, st
   // on the wide path the attention adds the QKV projection's partial sums itself
   QkvParts qp{};
   if (norm_proj(g, EPI_STORE, g.h(), hhi, hlo, md.wqkv(l), md.fqkv(l), 3 * d, d, g.qkv(), 3 * d, nullptr, s, err,
-                ss, &qp) != hipSuccess)
+                ss, c.lay.qcache ? nullptr : &qp) != hipSuccess)
     return hipErrorLaunchFailure;
-  TRY(attn_decode(dt, g.qkv(), g.lens(), jpos, B, m.n_heads, m.head_dim, c.lay.capacity, g.pages(), c.splits, c.rope(),
-                  g.kslab(l), g.vslab(l), g.part(), g.o(), s, olo, qp, B > 1 ? g.order() : nullptr));
-  if (c.splits > 1) TRY(attn_merge(dt, g.part(), B, m.n_heads, m.head_dim, c.splits, g.o(), s, olo));
+  if (c.lay.qcache) {
+    const QSegs sg{nullptr, nullptr, nullptr, g.lens(), jpos + 1, B, B, 1};
+    TRY(attn_qcache(c, c.qcache(l, g.r0, B), sg, c.lay.capacity, c.select, g.qkv(), true, g.o(), olo, s));
+  } else {
+    TRY(attn_decode(dt, g.qkv(), g.lens(), jpos, B, m.n_heads, m.head_dim, c.lay.capacity, g.pages(), c.splits, c.rope(),
+                    g.kslab(l), g.vslab(l), g.part(), g.o(), s, olo, qp, B > 1 ? g.order() : nullptr));
+    if (c.splits > 1) TRY(attn_merge(dt, g.part(), B, m.n_heads, m.head_dim, c.splits, g.o(), s, olo));
+  }
   TRY(resid_proj(g, g.o(), olo, md.wo(l), md.fo(l), d, hhi, hlo, s, ss));
   if (norm_proj(g, EPI_SWIGLU, g.h(), hhi, hlo, md.wgu(l), md.fgu(l), 2 * F, d, g.a(), F, alo, s, err, ss) != hipSuccess)
     return hipErrorLaunchFailure;
@@ -718,7 +750,7 @@ static bool graphs_enabled() {
 hipError_t ctx_decode(Ctx& c, int A, int32_t* tok, float* logits, const int32_t* forced, hipStream_t s,
                       std::string& err) {
   if (!graphs_enabled()) return enqueue_decode(c, A, tok, logits, forced, s, err);
-  GraphKey key{A, tok, logits, forced};
+  GraphKey key{A, tok, logits, forced, c.select};
   auto it = c.graphs.find(key);
   if (it == c.graphs.end()) {
     hipStream_t cs = c.capture_stream;

@@ -49,8 +49,10 @@ struct GraphKey {
   void* tokens;
   void* logits;
   const void* forced;
+  int select;
   bool operator<(const GraphKey& o) const {
-    return std::tie(n_actions, tokens, logits, forced) < std::tie(o.n_actions, o.tokens, o.logits, o.forced);
+    return std::tie(n_actions, tokens, logits, forced, select) <
+           std::tie(o.n_actions, o.tokens, o.logits, o.forced, o.select);
   }
 };
 
@@ -62,6 +64,7 @@ struct Ctx {
   int splits = 1;
   int fused_grid = 0;  // workgroups of the persistent decode, 0 when it does not apply
   int split_o = 1, split_d = 1, split_a = 1;
+  int select = 0;  // pages that each query of the action decode attends to (8-bit K/V), 0: all
   hipStream_t capture_stream = nullptr;
   // pinned host word the persistent decode sets when a barrier wait gives up
   // (host view, device view); read by the next call on the context
@@ -103,6 +106,14 @@ struct Ctx {
   int32_t* lens() const { return (int32_t*)(ws + lay.lens); }
   int32_t* meta() const { return (int32_t*)(ws + lay.meta); }
   int32_t* pt() const { return (int32_t*)(ws + lay.pt); }
+  // layer l's 8-bit K/V, for rows r0 .. r0 + rows - 1
+  QCache qcache(int l, int r0, int rows) const {
+    const Cfg& m = model->cfg;
+    return QCache{(uint8_t*)kslab(l), (uint8_t*)vslab(l), (float*)(ws + lay.qc_scale + (size_t)l * lay.scale_layer),
+                  (float*)(ws + lay.qc_scale + (size_t)(m.n_layers + l) * lay.scale_layer),
+                  (int8_t*)(ws + lay.qc_bound + (size_t)l * lay.bound_layer), pt() + (size_t)r0 * lay.ppr,
+                  lay.n_pages, m.n_heads, m.head_dim, rows, lay.ppr};
+  }
   KvPages pages() const { return KvPages{pt(), lay.ppr}; }
 };
 

@@ -17,6 +17,7 @@
 
 #include "fused_limits.h"
 #include "gemm_plan.h"
+#include "qcache_plan.h"
 
 namespace ams {
 
@@ -119,12 +120,24 @@ struct CtxLayout {
   bool share;
   int key_seg;  // segment size of the page keys (bytes)
   size_t hk_seg, hk_keys, hk_rows;
+  // 8-bit K/V (qcache): scales of K, then of V, [n_layers][n_pages][heads] fp32 each, key bounds
+  // [n_layers][n_pages][heads][2][head_dim], a decode pass's selected pages [B][heads][ppr] and the partial sums
+  // of its attention
+  bool qcache;
+  size_t qc_scale, qc_bound, qc_sel, qc_part, qc_part_floats;
+  size_t scale_layer, bound_layer;  // bytes of one layer's K (or V) scales, and of its bounds
   size_t xfer;  // host-tier transfer descriptors [batch] (16 bytes each)
 };
 
 // Bytes of the host image of a row of `len` positions (see the host tier).
 inline size_t row_host_bytes(const Cfg& c, int len) {
   return 256 + (size_t)2 * c.n_layers * len * c.d_model * elem_size(c) + (size_t)c.d_model * (4 + 2 + 2);
+}
+
+// The same for a context whose K/V are 8-bit caches: whole pages with their scales and bounds.
+inline size_t row_host_bytes_qcache(const Cfg& c, int len) {
+  const size_t unit = (size_t)130 * c.head_dim + 16, np = (len + 63) / 64;
+  return 256 + (size_t)c.n_layers * np * c.n_heads * unit + (size_t)c.d_model * (4 + 2 + 2);
 }
 
 inline int default_pass_tokens(int batch, int capacity) {
@@ -232,9 +245,10 @@ inline int check_ctx_args(const Cfg& c, int batch, int capacity, int pass_tokens
 }
 
 // n_pages: K/V pages per layer pool (0: batch * capacity / 64, a page for every
-// position of every row); share: rows may share prefix pages (hash scratch).
+// position of every row); share: rows may share prefix pages (hash scratch); qcache:
+// K/V in 8 bits.
 inline CtxLayout ctx_layout(const Cfg& c, int batch, int capacity, int pass_tokens, int n_pages = 0,
-                            bool share = false) {
+                            bool share = false, bool qcache = false) {
   CtxLayout x{};
   const size_t es = elem_size(c), d = c.d_model, F = c.d_ffn, L = c.n_layers, B = batch;
   x.batch = batch;
@@ -244,9 +258,20 @@ inline CtxLayout ctx_layout(const Cfg& c, int batch, int capacity, int pass_toke
   x.ppr = capacity / 64;
   x.n_pages = n_pages > 0 ? n_pages : batch * x.ppr;
   const size_t T = std::max<size_t>(x.pass_tokens, B);
-  x.slab_layer = (size_t)x.n_pages * 64 * d * es;
+  x.qcache = qcache;
+  x.slab_layer = (size_t)x.n_pages * 64 * d * (qcache ? 1 : es);
   size_t o = 0;
   x.kv = o; o = align256(o + 2 * L * x.slab_layer);
+  if (qcache) {  // (each layer's arrays 256-byte aligned)
+    x.scale_layer = align256((size_t)x.n_pages * c.n_heads * 4);
+    x.bound_layer = align256((size_t)x.n_pages * 2 * d);
+    x.qc_part_floats =
+        qcache_attend_plan(batch, c.n_heads, c.n_heads, c.head_dim, batch, 1, capacity, 0).part_floats;
+  }
+  x.qc_scale = o; o = align256(o + 2 * L * x.scale_layer);
+  x.qc_bound = o; o = align256(o + L * x.bound_layer);
+  x.qc_sel = o; o = align256(o + (qcache ? B * (size_t)c.n_heads * x.ppr * 4 : 0));
+  x.qc_part = o; o = align256(o + x.qc_part_floats * 4);
   x.h = o; o = align256(o + T * d * 4);
   x.u = o; o = align256(o + T * d * es);
   x.qkv = o; o = align256(o + T * 3 * d * 4);

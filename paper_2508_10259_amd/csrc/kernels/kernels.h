@@ -8,6 +8,7 @@
 
 #include "fused_limits.h"
 #include "gemm_plan.h"
+#include "qcache_plan.h"
 
 namespace ams {
 
@@ -318,15 +319,6 @@ struct QSegs {
 // rounded again when it grows.
 hipError_t qcache_append(const QCache& c, const QSegs& sg, const void* k, int64_t ldk, const void* v,
                          int64_t ldv, int dt, const float2* rope, hipStream_t s);
-// How an attention of such a call runs (qt column tiles of 16 per wave, `keys`: the waves share them), and the
-// floats of partial sums it needs.
-struct QAttendPlan {
-  bool keys;
-  int qt, tiles, splits;
-  size_t part_floats;
-};
-QAttendPlan qcache_attend_plan(int n_seg, int n_heads, int n_kv, int dh, int n_tok, int max_new, int max_len,
-                               int n_select);
 // Causal attention of the call's tokens over what their rows hold (after their append).  pair: queries and
 // probabilities as fp16 pairs.  sel: NULL, or the pages each token attends to [n_tok][H][n_sel]
 // (increasing, then -1).  olo: the rounding errors of an fp16 output, or NULL.
@@ -381,6 +373,13 @@ struct XferRow {
 hipError_t rows_xfer(bool to_host, const XferRow* rows, int n_rows, int L, int H, int dh, int es, void* pool,
                      size_t slab_layer, const int32_t* pt, int ppr, float* h_last, void* h16, void* h16lo, int d,
                      hipStream_t s);
+// The same for a context whose K/V are 8-bit caches (layer l: base + l * its strides): after the header, per
+// layer, page of the row (ceil(len / 64)) and head a unit of qcache_unit_bytes: the page's key codes [64][dh],
+// value codes [16][dh][4], bounds [2][dh], both scales and 8 bytes of padding; then the hidden state as above.
+constexpr size_t qcache_unit_bytes(int dh) { return (size_t)130 * dh + 16; }
+hipError_t rows_xfer_qcache(bool to_host, const XferRow* rows, int n_rows, int L, const QCache& first,
+                            size_t slab_layer, size_t scale_layer, size_t bound_layer, float* h_last, void* h16,
+                            void* h16lo, int d, hipStream_t s);
 
 // Flow-matching action head (flow.hip), over the n_tok tokens of a pass (x and
 // h of the pass's first token): flow_embed h[t] = W_in x[t] + tau w_t (W_in

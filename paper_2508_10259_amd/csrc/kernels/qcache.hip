@@ -1123,29 +1123,6 @@ hipError_t qcache_append(const QCache& c, const QSegs& sg, const void* k, int64_
   return hipGetLastError();
 }
 
-QAttendPlan qcache_attend_plan(int n_seg, int n_heads, int n_kv, int dh, int n_tok, int max_new, int max_len,
-                               int n_select) {
-  QAttendPlan p{};
-  const int G = n_heads / n_kv;
-  const int64_t cols = n_select ? G : (int64_t)max_new * G;
-  p.keys = n_select > 0 || cols <= 32;
-  p.qt = p.keys ? (cols <= 16 || n_select ? 1 : 2) : 2;
-  const int per = p.keys ? 16 * p.qt : 64 * p.qt;
-  p.tiles = (int)((cols + per - 1) / per);
-  // Splits: the last 32-position step of every workgroup ends at about the same time when there are
-  // some 1,024 of them (four per CU); a split keeps at least 2 steps for each of its waves.
-  const int64_t blocks = (int64_t)n_seg * n_kv * p.tiles * (n_select ? max_new : 1);
-  const int64_t positions = n_select ? (int64_t)n_select * PG : max_len;
-  const int64_t steps = (positions + 31) / 32, least = p.keys ? 8 : 16;
-  int64_t splits = (1024 + blocks - 1) / blocks;
-  splits = splits < (steps + least - 1) / least ? splits : (steps + least - 1) / least;
-  if (splits > 256) splits = 256;
-  if (splits < 1) splits = 1;
-  p.splits = (int)splits;
-  p.part_floats = splits > 1 ? (size_t)n_tok * n_heads * splits * (dh + 4) : 0;
-  return p;
-}
-
 template <int D, bool PAIR>
 static hipError_t attend_launch(const QAttendPlan& p, AttendArgs& a, hipStream_t s) {
   const unsigned pairs = (unsigned)a.sg.n_seg * a.c.H;

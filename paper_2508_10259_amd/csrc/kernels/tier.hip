@@ -3,7 +3,7 @@
 // rows between the K/V page pools and pinned host memory, written and read by
 // the kernels themselves through the host buffers' device addresses.
 //
-// Host image of a row (after a 256-byte header the host fills):
+// Host image of a row of fp16 or fp32 K/V (after a 256-byte header the host fills):
 //   K/V  [layer][K|V][head][len][head_dim]   compute type
 //   h_last [d] fp32, then its fp16 pair hi [d], lo [d]
 // One workgroup per (row, layer, K|V, head) moves that head's len x head_dim
@@ -59,7 +59,80 @@ __global__ __launch_bounds__(256) void k_rows_xfer(const XferRow* __restrict__ r
   }
 }
 
+// 8-bit contexts: a workgroup per (row, layer, head) moves that head's units (whole pages with their scales and
+// bounds), one more per row its hidden state.
+template <bool TO_HOST>
+__global__ __launch_bounds__(256) void k_rows_xfer_qcache(const XferRow* __restrict__ rows, int n_rows, int L, QCache c,
+                                                          size_t slab_layer, size_t scale_layer, size_t bound_layer,
+                                                          float* __restrict__ h_last, f16* __restrict__ h16,
+                                                          f16* __restrict__ h16lo, int d) {
+  const int per_row = L * c.H + 1;
+  const int i = blockIdx.x / per_row, k = blockIdx.x % per_row;
+  if (i >= n_rows) return;
+  const XferRow xr = rows[i];
+  const int np = (xr.len + KV_PAGE - 1) / KV_PAGE;
+  const size_t unit = qcache_unit_bytes(c.dh);
+  char* host = (char*)xr.host + 256;
+  if (k == L * c.H) {
+    float* hh = (float*)(host + (size_t)L * np * c.H * unit);
+    f16* hp = (f16*)(hh + d);
+    for (int e = threadIdx.x; e < d; e += blockDim.x) {
+      const size_t o = (size_t)xr.row * d + e;
+      if (TO_HOST) {
+        hh[e] = h_last[o];
+        hp[e] = h16[o];
+        hp[d + e] = h16lo[o];
+      } else {
+        h_last[o] = hh[e];
+        h16[o] = hp[e];
+        h16lo[o] = hp[d + e];
+      }
+    }
+    return;
+  }
+  const int l = k / c.H, h = k % c.H, codes = KV_PAGE * c.dh / 16, bounds = 2 * c.dh / 16;
+  const int per = 2 * codes + bounds + 1;  // 16-byte pieces of a unit
+  for (int q = threadIdx.x; q < np * per; q += blockDim.x) {
+    const int lp = q / per, e = q % per;
+    const size_t ph = (size_t)c.pt[(size_t)xr.row * c.ppr + lp] * c.H + h;
+    char* hq = host + (((size_t)l * np + lp) * c.H + h) * unit + (size_t)e * 16;
+    if (e == per - 1) {
+      float* ks = (float*)((char*)c.ks + l * scale_layer) + ph;
+      float* vs = (float*)((char*)c.vs + l * scale_layer) + ph;
+      float4* w = (float4*)hq;
+      if (TO_HOST) {
+        *w = float4{*ks, *vs, 0.f, 0.f};
+      } else {
+        const float4 x = *w;
+        *ks = x.x;
+        *vs = x.y;
+      }
+      continue;
+    }
+    uint4* dp;
+    if (e < codes) dp = (uint4*)(c.k + l * slab_layer + ph * KV_PAGE * c.dh) + e;
+    else if (e < 2 * codes) dp = (uint4*)(c.v + l * slab_layer + ph * KV_PAGE * c.dh) + (e - codes);
+    else dp = (uint4*)(c.kb + l * bound_layer + ph * 2 * c.dh) + (e - 2 * codes);
+    if (TO_HOST) *(uint4*)hq = *dp;
+    else *dp = *(uint4*)hq;
+  }
+}
+
 }  // namespace
+
+hipError_t rows_xfer_qcache(bool to_host, const XferRow* rows, int n_rows, int L, const QCache& first,
+                            size_t slab_layer, size_t scale_layer, size_t bound_layer, float* h_last, void* h16,
+                            void* h16lo, int d, hipStream_t s) {
+  if (n_rows <= 0) return hipSuccess;
+  const dim3 grid((unsigned)(n_rows * (L * first.H + 1)));
+  if (to_host)
+    hipLaunchKernelGGL(k_rows_xfer_qcache<true>, grid, dim3(256), 0, s, rows, n_rows, L, first, slab_layer,
+                       scale_layer, bound_layer, h_last, (f16*)h16, (f16*)h16lo, d);
+  else
+    hipLaunchKernelGGL(k_rows_xfer_qcache<false>, grid, dim3(256), 0, s, rows, n_rows, L, first, slab_layer,
+                       scale_layer, bound_layer, h_last, (f16*)h16, (f16*)h16lo, d);
+  return hipGetLastError();
+}
 
 hipError_t rows_xfer(bool to_host, const XferRow* rows, int n_rows, int L, int H, int dh, int es, void* pool,
                      size_t slab_layer, const int32_t* pt, int ppr, float* h_last, void* h16, void* h16lo, int d,

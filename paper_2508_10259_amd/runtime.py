@@ -139,13 +139,14 @@ class DeviceContext:
     """Per-row cached context: K/V slab + activations in one workspace."""
 
     def __init__(self, model: DeviceModel, batch: int, capacity: int, max_pass_tokens: int = 0,
-                 n_pages: Optional[int] = None, share_prefix: bool = False):
-        """n_pages / share_prefix: a paged context (ams_ctx_create_paged) with that many K/V pages per
-        layer (0: a page for every position) whose rows share prefix pages when share_prefix."""
+                 n_pages: Optional[int] = None, share_prefix: bool = False, qcache: bool = False):
+        """n_pages / share_prefix / qcache: a paged context (ams_ctx_create_paged) with that many K/V pages per
+        layer (0: a page for every position) whose rows share prefix pages when share_prefix, and whose
+        K/V are held in 8 bits when qcache."""
         self.lib, self.model, self.batch, self.capacity = model.lib, model, batch, capacity
         self.share_prefix = bool(share_prefix)
-        paged = n_pages is not None or share_prefix
-        flags = capi.AMS_CTX_SHARE_PREFIX if share_prefix else 0
+        paged = n_pages is not None or share_prefix or qcache
+        flags = (capi.AMS_CTX_SHARE_PREFIX if share_prefix else 0) | (capi.AMS_CTX_QCACHE if qcache else 0)
         if paged:
             nbytes = self.lib.ams_ctx_workspace_bytes_paged(C.byref(model.cfg), batch, capacity, max_pass_tokens,
                                                             n_pages or 0, flags)
@@ -222,6 +223,10 @@ class DeviceContext:
         capi.check(self.lib.ams_ctx_flow(self.handle, C.byref(head.c), x.data_ptr(), C.c_float(tau0), n_steps,
                                          _stream()), "ams_ctx_flow")
         return x
+
+    def select_pages(self, n_pages: int) -> None:
+        """Pages that each query of the action decode attends to (contexts with qcache; 0: all)."""
+        capi.check(self.lib.ams_ctx_select_pages(self.handle, n_pages), "ams_ctx_select_pages")
 
     def row_host_bytes(self, length: int) -> int:
         return int(self.lib.ams_ctx_row_host_bytes(self.handle, length))

@@ -103,3 +103,14 @@ def test_python_checks():
         c.attend_selected(x, off, lens, 2, selected=torch.zeros(3, 2, 3, dtype=torch.int32))
     with pytest.raises(ValueError):
         QuantCache(c.k, c.v, c.k_scale, c.v_scale[:2], c.k_bounds, c.page_table)
+
+
+def test_context_flags(lib):
+    from paper_2508_10259_amd.capi import AMS_CTX_QCACHE, AMS_CTX_SHARE_PREFIX, ModelCfg
+    cfg = C.byref(ModelCfg(4, 512, 4, 128, 1024, 256, 256, 1e-5, 1e4, 1))
+    size = [lib.ams_ctx_workspace_bytes_paged(cfg, 16, 1024, 0, 0, f) for f in
+            (0, AMS_CTX_QCACHE, AMS_CTX_SHARE_PREFIX, AMS_CTX_QCACHE | AMS_CTX_SHARE_PREFIX, 4, 7)]
+    kv = 4 * 2 * 16 * 1024 * 512 * 2
+    assert 0.44 * kv <= size[0] - size[1] <= 0.5 * kv and size[2] - size[3] == size[0] - size[1]
+    assert size[4] == size[5] == 0
+    assert lib.ams_ctx_select_pages(None, 1) == -1
