@@ -238,8 +238,9 @@ ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, co
                              int32_t max_new, const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t dtype,
                              void* stream);
 
-/* Bytes of device workspace ams_qcache_attend needs for these sizes (at least 1;
- * 0 if an argument is invalid).  Only the dimensions of `cache` are read. */
+/* Bytes of device workspace ams_qcache_attend needs for these sizes, whether it is
+ * given `selected` or not (1: none; 0 if an argument is invalid).  Only the
+ * dimensions of `cache` are read. */
 size_t ams_qcache_workspace_bytes(const ams_qcache* cache, int32_t n_heads, int32_t n_tok, int32_t max_new,
                                   int32_t max_len, int32_t n_select);
 
@@ -264,8 +265,8 @@ size_t ams_qcache_workspace_bytes(const ams_qcache* cache, int32_t n_heads, int3
  *           sums of whole numbers, so the choice does not depend on their order.
  *   selected: NULL, or device int32 [n_tok][n_kv_heads][n_select] receiving the
  *           chosen pages of the row in increasing order, then -1 (n_select > 0).
- *   ws:     device memory of ams_qcache_workspace_bytes, 16-byte aligned; used
- *           until the call has completed on its stream.
+ *   ws:     device memory of ams_qcache_workspace_bytes, 16-byte aligned (may be NULL
+ *           where that is 1); used until the call has completed on its stream.
  * fp16 and bf16: queries and probabilities enter the products as fp16, queries
  * scaled by a power of two first; fp32: as fp16 pairs (about 22 bits).  Statistics
  * and sums are fp32.  Errors: AMS_EINVAL, AMS_ENOMEM, AMS_ENODEV, AMS_EHIP. */

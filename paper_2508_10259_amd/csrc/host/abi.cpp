@@ -579,7 +579,7 @@ size_t ams_qcache_workspace_bytes(const ams_qcache* cache, int32_t n_heads, int3
   if (!qcache_sizes(cache, n_heads, n_tok, max_new, max_len, n_select, e)) return 0;
   if (n_tok == 0) return 1;
   const ams::QAttendPlan p = qcache_plan(cache, n_heads, n_tok, max_new, max_len, n_select);
-  return align16(p.part_floats * 4) + (size_t)n_tok * cache->n_kv_heads * n_select * 4 + 1;
+  return std::max<size_t>(1, align16(p.part_floats * 4) + (size_t)n_tok * cache->n_kv_heads * n_select * 4);
 }
 
 ams_status ams_qcache_attend(const ams_qcache* cache, const int32_t* tok_off, const int32_t* kv_len, int32_t n_tok,
@@ -600,16 +600,17 @@ ams_status ams_qcache_attend(const ams_qcache* cache, const int32_t* tok_off, co
       (int64_t)cache->rows * cache->n_kv_heads * p.tiles * p.splits * (n_select ? max_new : 1) > QCACHE_MAX_BLOCKS)
     return fail(AMS_EINVAL, "too many queries for one call: rows * max_new * n_heads is above 2^24");
   const size_t list = (size_t)n_tok * cache->n_kv_heads * n_select * 4, part = align16(p.part_floats * 4);
-  if (!ws) return fail(AMS_EINVAL, "ws is NULL");
+  const size_t need = part + (selected ? 0 : list);
+  if (need && !ws) return fail(AMS_EINVAL, "ws is NULL");
   if ((uintptr_t)ws & 15) return fail(AMS_EINVAL, "ws must be 16-byte aligned");
-  if (ws_bytes < part + list + 1) return fail(AMS_ENOMEM, "workspace too small: need " + std::to_string(part + list + 1));
+  if (ws_bytes < need) return fail(AMS_ENOMEM, "workspace too small: need " + std::to_string(need));
   if ((uintptr_t)selected & 3) return fail(AMS_EINVAL, "selected must be 4-byte aligned");
   int dev = 0;
   if (int s = current_device(&dev, e)) return fail(s, e);
   const int64_t width = (int64_t)n_heads * cache->head_dim;
   if (!qcache_arrays(cache, tok_off, kv_len, dev, e) || !qcache_tensor(q, ldq, n_tok, width, dtype, dev, "q", e) ||
       !qcache_tensor(out, ldo, n_tok, width, dtype, dev, "out", e) ||
-      !dev_range(ws, part + list + 1, dev, "ws", e) || (selected && !dev_range(selected, list, dev, "selected", e)))
+      (need && !dev_range(ws, need, dev, "ws", e)) || (selected && !dev_range(selected, list, dev, "selected", e)))
     return fail(AMS_EINVAL, e);
   const ams::QCache c = qcache_view(cache);
   const ams::QSegs sg{nullptr, tok_off, nullptr, kv_len, 0, cache->rows, n_tok, max_new};

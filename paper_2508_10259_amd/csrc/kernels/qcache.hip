@@ -58,11 +58,6 @@ __device__ __forceinline__ int page_of(const QCache& c, int row, int lp) {
   return (unsigned)p < (unsigned)c.n_pages ? p : -1;
 }
 
-// A scale, at a wave-uniform index; constant while an attention runs.
-__device__ __forceinline__ float scale_of(const float* p, size_t i) {
-  return __int_as_float(ld_const_uniform((const int32_t*)p, i));
-}
-
 // Eight consecutive elements of type dt (DType) as fp32; al: their address is 16-byte aligned.
 __device__ __forceinline__ void load8(const void* p, int64_t at, int dt, bool al, float* x) {
   if (dt == DT_F32) {
@@ -416,7 +411,7 @@ struct AttendArgs {
   float scale;
   const float2* rope;
   const int32_t* sel;  // [n_tok][H][n_sel] pages of a token's row (SEL)
-  int n_sel, tiles, splits;
+  int n_sel, tiles, splits, per, by_xcd;  // per: 32-position steps of a split
   float* part;
 };
 
@@ -424,52 +419,52 @@ template <int D> struct Step {  // a lane's K and V bytes of 32 positions
   uint4 k[2][D / 64], v[2][D / 64];
 };
 
-template <int D, bool NT>
+// (Plain loads: non-temporal ones cost 4% over 64 ragged rows and 36% where tokens select the same pages.)
+template <int D>
 __device__ __forceinline__ void load_k(const QCache& c, size_t ph, int half, int lane, uint4 (&k)[2][D / 64]) {
   const uint8_t* p = c.k + ph * (PG * D) + half * (32 * D) + (lane & 15) * D + (lane >> 4) * (D / 4);
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) {
-      const void* a = p + t * 16 * D + e * 16;
-      k[t][e] = NT ? ld_stream(a) : *(const uint4*)a;
-    }
+    for (int e = 0; e < D / 64; ++e) k[t][e] = *(const uint4*)(p + t * 16 * D + e * 16);
 }
-template <int D, bool NT>
+template <int D>
 __device__ __forceinline__ void load_v(const QCache& c, size_t ph, int half, int lane, uint4 (&v)[2][D / 64]) {
   const uint8_t* p = c.v + ph * (PG * D) + half * (32 * D) + (lane >> 4) * (4 * D) + (lane & 15) * (D / 4);
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) {
-      const void* a = p + t * 16 * D + e * 16;
-      v[t][e] = NT ? ld_stream(a) : *(const uint4*)a;
-    }
+    for (int e = 0; e < D / 64; ++e) v[t][e] = *(const uint4*)(p + t * 16 * D + e * 16);
 }
 
 template <int D, int QT, bool PAIR, bool KEYS, bool SEL>
-__global__ __launch_bounds__(256) void k_qcache_attend(AttendArgs a) {
+__global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendArgs a) {
   constexpr int NS = D / 32, NJ = D / 16, CT = 16 * QT;
   const QCache& c = a.c;
   // block -> (split, column tile, head, segment[, token])
   int id = blockIdx.x;
   int split, tile, h, s, tokn = 0;
-  if (KEYS) {
-    split = id % a.splits; id /= a.splits;
-    h = id % c.H; id /= c.H;
-    tile = id % a.tiles; id /= a.tiles;
-    if (SEL) { tokn = id % a.sg.max_new; id /= a.sg.max_new; }
-    s = id;
-  } else {
-    // the tiles of one (segment, head) pair follow each other on one XCD (blocks go to the 8 XCDs in
-    // turn), the longest first: they read the same pages through that XCD's L2
-    const int x = id & 7; id >>= 3;
+  if (a.by_xcd) {
+    // Blocks go to the 8 XCDs in turn; those of one (segment, head) pair follow each other on one XCD and
+    // read the same pages through its L2.  The tiles with the most positions go first.
+    const int x = id & 7;
+    id >>= 3;
     split = id % a.splits; id /= a.splits;
     tile = a.tiles - 1 - id % a.tiles; id /= a.tiles;
+    if (SEL) { tokn = id % a.sg.max_new; id /= a.sg.max_new; }
     const int pair = id * 8 + x;
     if (pair >= a.sg.n_seg * c.H) return;
     h = pair % c.H;
     s = pair / c.H;
+  } else {
+    // splits fastest, each (head, tile, ...) starting at another one: a short row's last splits have no work, and
+    // every XCD gets its share of those
+    split = id % a.splits; id /= a.splits;
+    split = (split + id) % a.splits;
+    h = id % c.H; id /= c.H;
+    if (SEL) { tokn = id % a.sg.max_new; id /= a.sg.max_new; }
+    tile = a.tiles - 1 - id % a.tiles; id /= a.tiles;
+    s = id;
   }
   Seg sg = seg_of(a.sg, s, c.rows, c.ppr * PG);
   if (SEL) {  // one token of the segment
@@ -485,6 +480,88 @@ __global__ __launch_bounds__(256) void k_qcache_attend(AttendArgs a) {
   if (blockcol >= ncols) return;
   const int col0 = KEYS ? blockcol : blockcol + wave * CT;
 
+  // what the wave's first and its last column see (a wave without columns: nothing)
+  const bool idle = col0 >= ncols;
+  const int vmin = idle ? 0 : max(sg.p0 + col0 / G + 1, 0);
+  const int vmax = idle ? 0 : max(sg.p0 + (min(col0 + CT, ncols) - 1) / G + 1, 0);
+
+  // 32-position steps of this split, and of this wave
+  const int32_t* list = SEL ? a.sel + ((size_t)sg.t0 * c.H + h) * a.n_sel : nullptr;
+  // (in KEYS mode every wave has the same columns; otherwise each stops at its own last position)
+  const int steps = SEL ? 2 * a.n_sel : (vmax + 31) / 32;
+  // (every row in chunks of the same length, so that the workgroups with work take as long as each other; the
+  // last split takes what a row has beyond the estimate)
+  const int begin = split * a.per, inc = KEYS ? 4 : 1;
+  const int end = split == a.splits - 1 ? steps : min(steps, begin + a.per);
+  // Lane j holds page, position and scales of the wave's j-th step from `from` on (a bit of `todo` each
+  // where there is a page), so that no step waits for the page table: one round trip for 64 steps.
+  int from = begin + (KEYS ? wave : 0), lane_page = 0, lane_pos = 0;
+  float lane_ks = 0.f, lane_vs = 0.f;
+  uint64_t todo = 0;
+  auto fill = [&] {
+    const int st = from + lane * inc;
+    bool ok = st < end;
+    if (ok) {
+      int lp = st >> 1;
+      if (SEL) lp = list[lp];
+      lane_pos = lp * PG + 32 * (st & 1);
+      // (a position at or behind vmax: the last page's second half)
+      ok = (unsigned)lp < (unsigned)c.ppr && lane_pos < vmax;
+      if (ok) {
+        lane_page = c.pt[(size_t)sg.row * c.ppr + lp];
+        ok = (unsigned)lane_page < (unsigned)c.n_pages;
+        if (ok) {
+          lane_ks = c.ks[(size_t)lane_page * c.H + h];
+          lane_vs = c.vs[(size_t)lane_page * c.H + h];
+        }
+      }
+    }
+    todo = __ballot(ok);
+  };
+
+  f32x4 o[QT][NJ];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // o is in units of 2^vref: a value page's scale relative to it goes into the conversion of its codes
+  int vref = 0;
+  bool first = true;
+
+  Step<D> x;
+  int pos = 0, npos = 0;
+  float ks = 0.f, vs = 0.f, nks = 0.f, nvs = 0.f;
+  size_t nph = 0;
+  bool more, nmore;
+  // the next step: its page and head, position and scales
+  auto next = [&] {
+    while (todo == 0) {
+      from += 64 * inc;
+      if (from >= end) {
+        nmore = false;
+        return;
+      }
+      fill();
+    }
+    const int j = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)todo) - 1);
+    todo &= todo - 1;
+    nph = (size_t)__builtin_amdgcn_readlane(lane_page, j) * c.H + h;
+    npos = __builtin_amdgcn_readlane(lane_pos, j);
+    nks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_ks), j));
+    nvs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_vs), j));
+    nmore = true;
+  };
+  fill();
+  next();
+  if (nmore) {
+    load_k<D>(c, nph, (npos >> 5) & 1, lane, x.k);
+    load_v<D>(c, nph, (npos >> 5) & 1, lane, x.v);
+  }
+  // (the first positions are on their way)
   // queries: scaled by a power of two so that a column's largest element is in [2^10, 2^11)
   half8 qh[QT][NS], ql[PAIR ? QT : 1][NS];
   float cq[QT];
@@ -537,90 +614,15 @@ __global__ __launch_bounds__(256) void k_qcache_attend(AttendArgs a) {
         if (PAIR) ql[t][k][e] = (f16)(y - (float)qh[t][k][e]);
       }
   }
-  // the columns' first and last visible positions of this wave
-  int vmin = 0x7FFFFFFF, vmax = 0;
-#pragma unroll
-  for (int t = 0; t < QT; ++t)
-    if (tokc[t] >= 0) {
-      vmin = min(vmin, vis[t]);
-      vmax = max(vmax, vis[t]);
-    }
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) {
-    vmin = min(vmin, __shfl_xor(vmin, o, 64));
-    vmax = max(vmax, __shfl_xor(vmax, o, 64));
-  }
-  vmin = __builtin_amdgcn_readfirstlane(vmin);
-  vmax = __builtin_amdgcn_readfirstlane(vmax);
-
-  // 32-position steps of this split, and of this wave
-  const int32_t* list = SEL ? a.sel + ((size_t)sg.t0 * c.H + h) * a.n_sel : nullptr;
-  int steps;
-  if (SEL) {
-    int lo = 0, up = a.n_sel;  // the entries before the first -1
-    while (lo < up) {
-      const int mid = (lo + up) >> 1;
-      if (ld_const_uniform(list, mid) >= 0) lo = mid + 1;
-      else up = mid;
-    }
-    steps = 2 * lo;
-  } else {
-    // (in KEYS mode every wave has the same columns; otherwise each stops at its own last position)
-    steps = (vmax + 31) / 32;
-  }
-  int all = steps;
-  if (!KEYS) {  // splits are the same for the workgroup's waves
-    const int lastcol = min(blockcol + 4 * CT, ncols) - 1;
-    all = (max(sg.p0 + lastcol / G + 1, 0) + 31) / 32;
-  }
-  const int per = (all + a.splits - 1) / a.splits;
-  const int begin = split * per, end = min(steps, begin + per), inc = KEYS ? 4 : 1;
-
-  f32x4 o[QT][NJ];
-  float m[QT], l[QT];
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    m[t] = -INFINITY;
-    l[t] = 0.f;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  // o is in units of 2^vref: a value page's scale relative to it goes into the conversion of its codes
-  int vref = 0;
-  bool first = true;
-
-  // the next step with a page in the pool: its page index and half
-  auto find = [&](int& st, size_t& ph, int& pos) {
-    for (; st < end; st += inc) {
-      int lp = st >> 1;
-      if (SEL) lp = ld_const_uniform(list, lp);
-      if (SEL && (unsigned)lp >= (unsigned)c.ppr) continue;
-      const int page = page_of(c, sg.row, lp);
-      if (page < 0) continue;
-      ph = (size_t)page * c.H + h;
-      pos = lp * PG + 32 * (st & 1);
-      if (pos >= vmax) continue;  // the last page's second half
-      return true;
-    }
-    return false;
-  };
-
-  Step<D> x;
-  int st = begin + (KEYS ? wave : 0), pos = 0;
-  size_t ph = 0;
-  bool more = find(st, ph, pos);
-  if (more) {
-    load_k<D, KEYS>(c, ph, (pos >> 5) & 1, lane, x.k);
-    load_v<D, KEYS>(c, ph, (pos >> 5) & 1, lane, x.v);
-  }
+  more = nmore;
+  pos = npos;
+  ks = nks;
+  vs = nvs;
   // One step; EDGE: some of its positions are masked for a column, or lie behind the row's last one.
   auto step = [&](auto edge_tag) {
     constexpr bool EDGE = decltype(edge_tag)::value;
-    const float ks = scale_of(c.ks, ph), vs = scale_of(c.vs, ph);
     const int p0 = pos;
-    int nst = st + inc, npos = 0;
-    size_t nph = 0;
-    const bool nmore = find(nst, nph, npos);
+    next();
     // S^T = K Q^T
     f32x4 sc[QT][2];
 #pragma unroll
@@ -637,7 +639,7 @@ __global__ __launch_bounds__(256) void k_qcache_attend(AttendArgs a) {
           if (PAIR) sc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, ql[t][k], sc[t][n], 0, 0, 0);
         }
       }
-    if (nmore) load_k<D, KEYS>(c, nph, (npos >> 5) & 1, lane, x.k);
+    if (nmore) load_k<D>(c, nph, (npos >> 5) & 1, lane, x.k);
     // softmax of the 32 positions
     int ve = exponent_of(vs);
     if (first) vref = ve;
@@ -709,11 +711,11 @@ __global__ __launch_bounds__(256) void k_qcache_attend(AttendArgs a) {
         if (PAIR) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, pl8[t], o[t][j], 0, 0, 0);
       }
     }
-    if (nmore) load_v<D, KEYS>(c, nph, (npos >> 5) & 1, lane, x.v);
-    st = nst;
-    ph = nph;
-    pos = npos;
+    if (nmore) load_v<D>(c, nph, (npos >> 5) & 1, lane, x.v);
     more = nmore;
+    pos = npos;
+    ks = nks;
+    vs = nvs;
   };
   // (positions increase, so the steps at the edge are the last ones; vmin <= len)
   while (more && pos + 32 <= vmin) step(std::false_type{});
@@ -843,18 +845,39 @@ __global__ __launch_bounds__(256) void k_qcache_join(AttendArgs a) {
   if (tokn >= sg.n) return;
   const int tok = sg.t0 + tokn;
   const float* p = a.part + ((size_t)tok * heads + head) * a.splits * LD;
-  float M = -INFINITY;
-  for (int k = lane; k < a.splits; k += 64) M = fmaxf(M, p[(size_t)k * LD + D]);
-  M = wave_max(M);
-  float L = 0.f, y[E];
+  // The first splits' sums are on their way before their factors are known: a launch of this size is all
+  // latency.  Lane k holds the factor of split k0 + k.
+  constexpr int PRE = 16;
+  float pre[PRE][E];
+#pragma unroll
+  for (int k = 0; k < PRE; ++k)
+#pragma unroll
+    for (int e = 0; e < E; ++e) pre[k][e] = p[(size_t)min(k, a.splits - 1) * LD + lane * E + e];
+  float M = -INFINITY, L = 0.f, y[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) y[e] = 0.f;
-  for (int k = 0; k < a.splits; ++k) {
-    const float* q = p + (size_t)k * LD;
-    const float mk = q[D], f = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk - M);
-    L += q[D + 1] * f;
+  for (int k = lane; k < a.splits; k += 64) M = fmaxf(M, p[(size_t)k * LD + D]);
+  M = wave_max(M);
+  auto factor = [](float f, int k) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), k)); };
+  for (int k0 = 0; k0 < a.splits; k0 += 64) {
+    float f = 0.f, l = 0.f;
+    if (k0 + lane < a.splits) {
+      const float* q = p + (size_t)(k0 + lane) * LD + D;
+      f = q[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(q[0] - M);
+      l = q[0] == -INFINITY ? 0.f : q[1] * f;
+    }
+    L += wave_sum(l);
+    const int n = min(a.splits - k0, 64);
+    const float* q = p + (size_t)k0 * LD + lane * E;
+    if (k0 == 0)
 #pragma unroll
-    for (int e = 0; e < E; ++e) y[e] += q[lane * E + e] * f;
+      for (int k = 0; k < PRE; ++k)  // (the factor of a split that is not there is 0, its sums are another's)
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] += k < n ? pre[k][e] * factor(f, k) : 0.f;
+#pragma unroll 8
+    for (int k = k0 == 0 ? PRE : 0; k < n; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = fmaf(q[(size_t)k * LD + e], factor(f, k), y[e]);
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
   const int64_t at = (int64_t)tok * a.ldo + (int64_t)head * D + lane * E;
@@ -876,8 +899,9 @@ __global__ __launch_bounds__(256) void k_qcache_join(AttendArgs a) {
 // its keys, from each channel's largest and smallest key, in whole numbers (|q^| <= 127 times bounds of
 // at most 112, 128 channels: below 2^21), so it has the same bits in any order of summation:
 //   2^ke max over heads of sum_d max(q^_d, 0) hi_d + min(q^_d, 0) lo_d
-// as one 8-bit product of [q^+ | q^-] (a head per column) with the bounds' rows [hi | lo] (a page per row).
-// Then the n_sel best: the threshold by four 8-bit digits of the keys' order, ties to the lower page.
+// as one 8-bit product of [q^+ | q^-] (a head per row) with the bounds [hi | lo] (a page per column).
+// Then the n_sel best, ties to the lower page: up to 1,024 pages by one wave, more by four 8-bit digits of the
+// keys' order.
 
 struct SelectArgs {
   QCache c;
@@ -891,9 +915,41 @@ struct SelectArgs {
 
 constexpr int SEL_OUT = 0;  // the key of a page that cannot be chosen; every other key is larger
 
+// The n_sel best of np <= 64 N keys by one wave, N keys to a lane: the key of rank n_sel bit by bit, counts in the
+// scalar unit .
+template <int N>
+__device__ __forceinline__ void select_wave(const uint32_t* key, int np, int n_sel, int lane, int32_t* out) {
+  uint32_t k[N], T = 0u;
+  int count = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) k[j] = j * 64 + lane < np ? key[j * 64 + lane] : 0u;
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t t = T | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) n += (int)__popcll(__ballot(k[j] >= t));
+    if (n >= n_sel) T = t;
+    if (n == n_sel) break;
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) count += (int)__popcll(__ballot(k[j] > T));
+  int need = T == (uint32_t)SEL_OUT ? 0 : n_sel - count, at = 0;  // how many of T itself
+  const uint64_t below = (1ull << lane) - 1ull;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const uint64_t same = __ballot(k[j] == T);
+    const bool take = k[j] > T || (k[j] == T && (int)__popcll(same & below) < need);
+    const uint64_t taken = __ballot(take);
+    if (take) out[at + (int)__popcll(taken & below)] = j * 64 + lane;
+    at += (int)__popcll(taken);
+    need -= min(need, (int)__popcll(same));
+  }
+  for (int p = at + lane; p < n_sel; p += 64) out[p] = -1;
+}
+
 template <int D, int NT>
 __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
-  constexpr int NW = NT / 64, NB = 2 * D / 64;
+  constexpr int NW = NT / 64, NB = 2 * D / 64, U = 4;
   extern __shared__ uint32_t key[];  // [ppr]
   __shared__ uint32_t hist[256];
   __shared__ uint32_t pick[2];
@@ -911,6 +967,26 @@ __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
   int32_t* out = a.sel + ((size_t)tok * c.H + h) * a.n_sel;
 
   if (np > a.n_sel) {
+    // U groups of 16 pages at a time, so that a wave waits twice (page table, bounds) and not twice for each;
+    // the first ones are on their way while the queries are
+    int page[U];
+    float ks[U];
+    i32x4 bound[U][NB];
+    auto fetch = [&](int p0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) page[u] = c.pt[(size_t)sg.row * c.ppr + min(p0 + u * NW * 16 + i, np - 1)];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool ok = (unsigned)page[u] < (unsigned)c.n_pages;
+        const size_t ph = (size_t)(ok ? page[u] : 0) * c.H + h;
+        const i32x4* b = (const i32x4*)(c.kb + ph * (2 * D)) + g;
+        page[u] = ok ? page[u] : -1;
+        ks[u] = c.ks[ph];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) bound[u][n] = b[4 * n];
+      }
+    };
+    fetch(wave * 16);
     // the largest |q| of the group's heads; lane (i, g) reads head i's channels 64 b + 16 g .. of each
     // block b of 64 (all waves the same)
     auto load16 = [&](int col, int b, float* x) {
@@ -966,48 +1042,39 @@ __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
         B[b] = up;
         B[b + D / 64] = dn;
       }
-      for (int p0 = wave * 16; p0 < np; p0 += NW * 16) {
-        const int lp = p0 + i;
-        int page = -1;
-        if (lp < np) {
-          page = c.pt[(size_t)sg.row * c.ppr + lp];
-          if ((unsigned)page >= (unsigned)c.n_pages) page = -1;
-        }
-        i32x4 acc = {0, 0, 0, 0};
-        float ks = 0.f;
-        i32x4 A[NB];
-        if (page >= 0) {
-          const size_t ph = (size_t)page * c.H + h;
-          ks = c.ks[ph];
-          const i32x4* b = (const i32x4*)(c.kb + ph * (2 * D)) + g;
+      // heads as rows, pages as columns: a lane's sums are those of its page
+      for (int p0 = wave * 16; p0 < np; p0 += NW * 16 * U) {
+        if (c0 > 0 || p0 != wave * 16) fetch(p0);
 #pragma unroll
-          for (int n = 0; n < NB; ++n) A[n] = b[4 * n];
-        } else {
+        for (int u = 0; u < U; ++u) {
+          i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-          for (int n = 0; n < NB; ++n) A[n] = i32x4{0, 0, 0, 0};
-        }
+          for (int n = 0; n < NB; ++n) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(B[n], bound[u][n], acc, 0, 0, 0);
+          int v = INT_MIN;
 #pragma unroll
-        for (int n = 0; n < NB; ++n) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(A[n], B[n], acc, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          int v = col < G ? acc[r] : INT_MIN;
-#pragma unroll
-          for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor(v, o, 64));
-          const float sk = __shfl(ks, 4 * g + r, 64);
-          const int there = __shfl(page, 4 * g + r, 64);
-          const int lpr = p0 + 4 * g + r;
-          if (i == 0 && lpr < np) {
-            uint32_t u = __float_as_uint((float)v * sk);
-            if (u == 0x80000000u) u = 0u;
-            u = u & 0x80000000u ? ~u : u | 0x80000000u;
-            if (lpr == np - 1) u = 0xFFFFFFFFu;
-            if (there < 0) u = SEL_OUT;
-            key[lpr] = c0 ? max(key[lpr], u) : u;
+          for (int r = 0; r < 4; ++r)
+            if (c0 + 4 * g + r < G) v = max(v, acc[r]);
+          v = max(v, __shfl_xor(v, 16, 64));
+          v = max(v, __shfl_xor(v, 32, 64));
+          const int lp = p0 + u * NW * 16 + i;
+          if (g == 0 && lp < np) {
+            uint32_t k = __float_as_uint((float)v * ks[u]);
+            k = k & 0x80000000u ? ~k : k | 0x80000000u;
+            if (lp == np - 1) k = 0xFFFFFFFFu;
+            if (page[u] < 0) k = SEL_OUT;
+            key[lp] = c0 ? max(key[lp], k) : k;
           }
         }
       }
     }
     __syncthreads();
+    if (np <= 1024) {
+      if (wave) return;
+      if (np <= 64) select_wave<1>(key, np, a.n_sel, lane, out);
+      else if (np <= 256) select_wave<4>(key, np, a.n_sel, lane, out);
+      else select_wave<16>(key, np, a.n_sel, lane, out);
+      return;
+    }
     // the key of rank n_sel: digit by digit, `need` of the keys with the digits so far are wanted
     uint32_t prefix = 0u, need = a.n_sel;
     for (int d = 24; d >= 0; d -= 8) {
@@ -1126,14 +1193,11 @@ hipError_t qcache_append(const QCache& c, const QSegs& sg, const void* k, int64_
 template <int D, bool PAIR>
 static hipError_t attend_launch(const QAttendPlan& p, AttendArgs& a, hipStream_t s) {
   const unsigned pairs = (unsigned)a.sg.n_seg * a.c.H;
-  if (a.sel) {
-    k_qcache_attend<D, 1, PAIR, true, true><<<pairs * p.tiles * p.splits * a.sg.max_new, 256, 0, s>>>(a);
-  } else if (p.keys) {
-    if (p.qt == 1) k_qcache_attend<D, 1, PAIR, true, false><<<pairs * p.tiles * p.splits, 256, 0, s>>>(a);
-    else k_qcache_attend<D, 2, PAIR, true, false><<<pairs * p.tiles * p.splits, 256, 0, s>>>(a);
-  } else {
-    k_qcache_attend<D, 2, PAIR, false, false><<<(pairs + 7) / 8 * 8 * p.tiles * p.splits, 256, 0, s>>>(a);
-  }
+  const unsigned grid = (a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * p.tiles * p.splits * (a.sel ? a.sg.max_new : 1);
+  if (a.sel) k_qcache_attend<D, 1, PAIR, true, true><<<grid, 256, 0, s>>>(a);
+  else if (!p.keys) k_qcache_attend<D, 2, PAIR, false, false><<<grid, 256, 0, s>>>(a);
+  else if (p.qt == 1) k_qcache_attend<D, 1, PAIR, true, false><<<grid, 256, 0, s>>>(a);
+  else k_qcache_attend<D, 2, PAIR, true, false><<<grid, 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const size_t items = (size_t)a.sg.n_seg * a.sg.max_new * a.c.H * a.G;
@@ -1145,8 +1209,13 @@ hipError_t qcache_attend(const QCache& c, const QSegs& sg, const QAttendPlan& p,
                          const void* q, int64_t ldq, int dt, bool pair, float scale, const float2* rope,
                          const int32_t* sel, int n_sel, void* o, int64_t ldo, int odt, void* olo, float* part,
                          hipStream_t s) {
+  // Several workgroups that read the same pages share an L2 where that leaves no XCD idle: with a multiple of 8
+  // pairs, or many.
+  const int pairs = sg.n_seg * c.H;
+  const bool shared = p.tiles > 1 || (sel && sg.max_new > 1);
+  const int by_xcd = shared && (pairs % 8 == 0 || pairs >= 64);
   AttendArgs a{c, sg, q, ldq, o, ldo, (f16*)olo, dt, odt, aligned16(q, ldq, type_bytes(dt)),
-               aligned16(o, ldo, type_bytes(odt)), n_heads / c.H, scale, rope, sel, n_sel, p.tiles, p.splits, part};
+               aligned16(o, ldo, type_bytes(odt)), n_heads / c.H, scale, rope, sel, n_sel, p.tiles, p.splits, p.per, by_xcd, part};
   if (c.dh == 128) return pair ? attend_launch<128, true>(p, a, s) : attend_launch<128, false>(p, a, s);
   return pair ? attend_launch<64, true>(p, a, s) : attend_launch<64, false>(p, a, s);
 }
@@ -1169,7 +1238,7 @@ hipError_t qcache_select(const QCache& c, const QSegs& sg, int n_heads, const vo
   const unsigned grid = (unsigned)sg.n_seg * c.H * sg.max_new;
   if (c.ppr <= 256)
     return c.dh == 128 ? select_launch<128, 256>(a, grid, s) : select_launch<64, 256>(a, grid, s);
-  return c.dh == 128 ? select_launch<128, 1024>(a, grid, s) : select_launch<64, 1024>(a, grid, s);
+  return c.dh == 128 ? select_launch<128, 512>(a, grid, s) : select_launch<64, 512>(a, grid, s);
 }
 
 }  // namespace ams

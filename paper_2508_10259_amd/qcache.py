@@ -7,6 +7,7 @@ replayed.  Everything runs on torch's current stream.
 """
 from __future__ import annotations
 
+import ctypes as C
 import math
 from typing import Optional, Tuple
 
@@ -17,6 +18,10 @@ from . import capi
 PAGE = 64
 E4M3 = torch.float8_e4m3fn
 _DTYPES = {torch.float32: capi.AMS_F32, torch.bfloat16: capi.AMS_BF16, torch.float16: capi.AMS_F16}
+
+
+def _raw_stream(index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _want(ok: bool, what: str) -> None:
@@ -45,13 +50,19 @@ class QuantCache:
             _want(tuple(t.shape) == shape and t.dtype == dtype and t.is_contiguous() and t.device == k.device,
                   f"{name} must be a contiguous {dtype} tensor of shape {shape} on {k.device}")
         _want(page_table.dim() == 2, "page_table must be [rows, pages_per_row]")
-        self.lib = capi.load()
+        self.lib = lib = capi.load()
         self.k, self.v, self.k_scale, self.v_scale, self.k_bounds = k, v, k_scale, v_scale, k_bounds
         self.page_table = page_table
         self.n_kv_heads, self.head_dim, self.rows = heads, dim, page_table.shape[0]
         self.device = k.device
         self.c = capi.QCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_bounds.data_ptr(),
                              page_table.data_ptr(), pages, heads, dim, self.rows, page_table.shape[1])
+        # (a decode step makes these calls for every layer, so what does not change is kept)
+        self._ref = C.byref(self.c)
+        self._append, self._attend, self._workspace = \
+            lib.ams_qcache_append, lib.ams_qcache_attend, lib.ams_qcache_workspace_bytes
+        self._index = 0 if k.device.index is None else k.device.index
+        self._off_shape, self._len_shape = torch.Size((self.rows + 1,)), torch.Size((self.rows,))
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_table: torch.Tensor) -> "QuantCache":
@@ -63,18 +74,23 @@ class QuantCache:
                    torch.zeros(n_pages, n_kv_heads, 2, head_dim, dtype=torch.int8, device=dev), page_table)
 
     def _rows(self, tok_off: torch.Tensor, lens: torch.Tensor) -> None:
-        _want(tok_off.dtype == torch.int32 and tok_off.is_contiguous() and tok_off.numel() == self.rows + 1
-              and tok_off.device == self.device, "tok_off must be a contiguous int32 tensor [rows + 1] of the cache's device")
-        _want(lens.dtype == torch.int32 and lens.is_contiguous() and lens.numel() == self.rows
-              and lens.device == self.device, "lens must be a contiguous int32 tensor [rows] of the cache's device")
+        if tok_off.dtype != torch.int32 or tok_off.shape != self._off_shape or not tok_off.is_contiguous() \
+                or tok_off.device != self.device:
+            raise ValueError("tok_off must be a contiguous int32 tensor [rows + 1] of the cache's device")
+        if lens.dtype != torch.int32 or lens.shape != self._len_shape or not lens.is_contiguous() \
+                or lens.device != self.device:
+            raise ValueError("lens must be a contiguous int32 tensor [rows] of the cache's device")
 
     def _tensor(self, t: torch.Tensor, name: str) -> int:
         """Token stride of a [n_tok, heads, head_dim] tensor whose heads lie one after another."""
-        _want(t.dim() == 3 and t.shape[2] == self.head_dim and t.dtype in _DTYPES and t.device == self.device,
-              f"{name} must be a float32, bfloat16 or float16 tensor [n_tok, heads, {self.head_dim}] of the cache's device")
-        _want(t.numel() == 0 or (t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == self.head_dim)),
-              f"{name}: the heads of a token must lie one after another")
-        return t.stride(0) if t.shape[0] > 1 else t.shape[1] * self.head_dim
+        shape, stride, dim = t.shape, t.stride(), self.head_dim
+        if len(shape) != 3 or shape[2] != dim or t.dtype not in _DTYPES or t.device != self.device:
+            raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor [n_tok, heads, {dim}] of the cache's "
+                             "device")
+        n, heads, _ = shape
+        if n * heads and (stride[2] != 1 or (heads > 1 and stride[1] != dim)):
+            raise ValueError(f"{name}: the heads of a token must lie one after another")
+        return stride[0] if n > 1 else heads * dim
 
     def append(self, k: torch.Tensor, v: torch.Tensor, tok_off: torch.Tensor, lens: torch.Tensor, *,
                max_new: Optional[int] = None) -> None:
@@ -84,19 +100,19 @@ class QuantCache:
         self._rows(tok_off, lens)
         ldk, ldv = self._tensor(k, "k"), self._tensor(v, "v")
         n = k.shape[0]
-        _want(k.shape == v.shape and k.shape[1] == self.n_kv_heads and k.dtype == v.dtype,
-              "k and v must have the cache's heads, one shape and one type")
-        capi.check(self.lib.ams_qcache_append(self.c, tok_off.data_ptr(), lens.data_ptr(), n,
-                                              max(n, 1) if max_new is None else max_new, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                                              _DTYPES[k.dtype], torch.cuda.current_stream().cuda_stream),
-                   "ams_qcache_append")
+        if k.shape != v.shape or k.shape[1] != self.n_kv_heads or k.dtype != v.dtype:
+            raise ValueError("k and v must have the cache's heads, one shape and one type")
+        status = self._append(self._ref, tok_off.data_ptr(), lens.data_ptr(), n, max(n, 1) if max_new is None else max_new,
+                              k.data_ptr(), ldk, v.data_ptr(), ldv, _DTYPES[k.dtype], _raw_stream(self._index))
+        if status:
+            capi.check(status, "ams_qcache_append")
 
     def attend(self, q: torch.Tensor, tok_off: torch.Tensor, lens: torch.Tensor, *, max_new: Optional[int] = None,
                max_len: Optional[int] = None, scale: Optional[float] = None,
                out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Causal attention of the tokens' queries [n_tok, n_heads, head_dim] over everything their rows hold.
         max_len: about the longest row (default: the capacity); scale: default 1 / sqrt(head_dim)."""
-        return self._attend(q, tok_off, lens, 0, max_new, max_len, scale, out, None)
+        return self._run(q, tok_off, lens, 0, max_new, max_len, scale, out, None)
 
     def attend_selected(self, q: torch.Tensor, tok_off: torch.Tensor, lens: torch.Tensor, n_select: int, *,
                         max_new: Optional[int] = None, max_len: Optional[int] = None, scale: Optional[float] = None,
@@ -104,31 +120,39 @@ class QuantCache:
                         selected: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """The same over n_select pages of each token and KV head.  Returns (out, selected): the chosen
         pages of the row [n_tok, kv heads, n_select] int32, increasing, then -1."""
-        _want(n_select >= 1, "n_select must be >= 1")
+        if n_select < 1:
+            raise ValueError("n_select must be >= 1")
         if selected is None:
             selected = torch.empty((q.shape[0], self.n_kv_heads, n_select), dtype=torch.int32, device=self.device)
-        _want(selected.dtype == torch.int32 and selected.is_contiguous() and selected.device == self.device
-              and tuple(selected.shape) == (q.shape[0], self.n_kv_heads, n_select),
-              "selected must be a contiguous int32 tensor [n_tok, kv heads, n_select] of the cache's device")
-        return self._attend(q, tok_off, lens, n_select, max_new, max_len, scale, out, selected), selected
+        elif selected.dtype != torch.int32 or not selected.is_contiguous() or selected.device != self.device \
+                or tuple(selected.shape) != (q.shape[0], self.n_kv_heads, n_select):
+            raise ValueError("selected must be a contiguous int32 tensor [n_tok, kv heads, n_select] of the cache's device")
+        return self._run(q, tok_off, lens, n_select, max_new, max_len, scale, out, selected), selected
 
-    def _attend(self, q, tok_off, lens, n_select, max_new, max_len, scale, out, selected):
+    def _run(self, q, tok_off, lens, n_select, max_new, max_len, scale, out, selected):
         self._rows(tok_off, lens)
-        ldq, (n, heads, _) = self._tensor(q, "q"), q.shape
+        ldq = self._tensor(q, "q")
+        n, heads, dim = q.shape
         if out is None:
-            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
-        ldo = self._tensor(out, "out")
-        _want(out.shape == q.shape and out.dtype == q.dtype, "out must have q's shape and type")
+            out = torch.empty((n, heads, dim), dtype=q.dtype, device=self.device)
+            ldo = heads * dim
+        else:
+            ldo = self._tensor(out, "out")
+            if out.shape != q.shape or out.dtype != q.dtype:
+                raise ValueError("out must have q's shape and type")
         if max_new is None:
             max_new = max(n, 1)
         if max_len is None:
-            max_len = self.page_table.shape[1] * PAGE
-        need = self.lib.ams_qcache_workspace_bytes(self.c, heads, n, max_new, max_len, n_select)
-        # from the allocator at every call: its memory follows the stream, and a captured graph's stays with it
-        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=self.device)
-        capi.check(self.lib.ams_qcache_attend(
-            self.c, tok_off.data_ptr(), lens.data_ptr(), n, max_new, max_len, heads, q.data_ptr(), ldq, out.data_ptr(),
-            ldo, _DTYPES[q.dtype], 1 / math.sqrt(self.head_dim) if scale is None else scale, n_select,
-            selected.data_ptr() if selected is not None else None, ws.data_ptr(), ws.numel(),
-            torch.cuda.current_stream().cuda_stream), "ams_qcache_attend")
+            max_len = self.c.pages_per_row * PAGE
+        ws, need = None, self._workspace(self._ref, heads, n, max_new, max_len, n_select)
+        if need > 1:
+            # from the allocator at every call: its memory follows the stream, and a captured graph's stays with it
+            ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        status = self._attend(
+            self._ref, tok_off.data_ptr(), lens.data_ptr(), n, max_new, max_len, heads, q.data_ptr(), ldq, out.data_ptr(),
+            ldo, _DTYPES[q.dtype], 1 / math.sqrt(dim) if scale is None else scale, n_select,
+            None if selected is None else selected.data_ptr(), None if ws is None else ws.data_ptr(), need,
+            _raw_stream(self._index))
+        if status:
+            capi.check(status, "ams_qcache_attend")
         return out

@@ -52,7 +52,8 @@ def test_append_arguments(lib, bad):
 @pytest.mark.parametrize("bad", [dict(n_tok=-1), dict(max_new=0), dict(max_len=0), dict(n_heads=3), dict(n_heads=0),
                                  dict(dtype=5), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
                                  dict(scale=float("inf")), dict(n_select=-1), dict(n_select=16385),
-                                 dict(selected=64), dict(ws=None), dict(ws=4104), dict(n_select=2, selected=66)])
+                                 dict(selected=64), dict(ws=None, n_select=2), dict(ws=4104),
+                                 dict(n_select=2, selected=66)])
 def test_attend_arguments(lib, bad):
     assert _attend(lib, _cache(), **bad) == -1
 
