@@ -596,8 +596,7 @@ ams_status ams_qcache_attend(const ams_qcache* cache, const int32_t* tok_off, co
   const ams::QAttendPlan p = qcache_plan(cache, n_heads, n_tok, max_new, max_len, n_select);
   max_new = std::min(max_new, n_tok);
   const int64_t heads = (int64_t)cache->rows * n_heads * max_new;
-  if (heads > 4 * QCACHE_MAX_BLOCKS ||
-      (int64_t)cache->rows * cache->n_kv_heads * p.tiles * p.splits * (n_select ? max_new : 1) > QCACHE_MAX_BLOCKS)
+  if (heads > 4 * QCACHE_MAX_BLOCKS || p.blocks > QCACHE_MAX_BLOCKS)
     return fail(AMS_EINVAL, "too many queries for one call: rows * max_new * n_heads is above 2^24");
   const size_t list = (size_t)n_tok * cache->n_kv_heads * n_select * 4, part = align16(p.part_floats * 4);
   const size_t need = part + (selected ? 0 : list);

@@ -34,18 +34,20 @@ constexpr float QC_LOG2E = 1.4426950408889634f;
 struct Seg {
   int row, t0, n, p0, len;
 };
+template <bool UNIFORM = true>  // whether s is the same for the whole wave
 __device__ __forceinline__ Seg seg_of(const QSegs& sg, int s, int rows, int cap) {
+  auto at = [](const int32_t* p, int k) { return UNIFORM ? ld_const_uniform(p, k) : p[k]; };
   Seg x;
-  x.row = sg.row ? ld_const_uniform(sg.row, s) : s;
-  x.t0 = sg.off ? ld_const_uniform(sg.off, s) : s;
-  const int t1 = sg.off ? ld_const_uniform(sg.off, s + 1) : s + 1;
+  x.row = sg.row ? at(sg.row, s) : s;
+  x.t0 = sg.off ? at(sg.off, s) : s;
+  const int t1 = sg.off ? at(sg.off, s + 1) : s + 1;
   x.t0 = min(max(x.t0, 0), sg.n_tok);
   x.n = min(min(max(t1, x.t0), sg.n_tok) - x.t0, sg.max_new);
   if (sg.pos) {
-    x.p0 = ld_const_uniform(sg.pos, s);
+    x.p0 = at(sg.pos, s);
     x.len = min(max(x.p0, -sg.n_tok) + x.n, cap);
   } else {
-    x.len = min(max(ld_const_uniform(sg.len, s), 0) + sg.len_add, cap);
+    x.len = min(max(at(sg.len, s), 0) + sg.len_add, cap);
   }
   x.p0 = x.len - x.n;
   if (x.row < 0 || x.row >= rows) x.n = 0;
@@ -412,6 +414,7 @@ struct AttendArgs {
   const float2* rope;
   const int32_t* sel;  // [n_tok][H][n_sel] pages of a token's row (SEL)
   int n_sel, tiles, splits, per, by_xcd;  // per: 32-position steps of a split
+  bool even;  // the segments' lengths set it instead (even_steps)
   float* part;
 };
 
@@ -437,14 +440,55 @@ __device__ __forceinline__ void load_v(const QCache& c, size_t ph, int half, int
     for (int e = 0; e < D / 64; ++e) v[t][e] = *(const uint4*)(p + t * 16 * D + e * 16);
 }
 
+// The 32-position steps that segment s's last token sees.
+__device__ __forceinline__ int steps_of(const AttendArgs& a, int s) {
+  if (s >= a.sg.n_seg) return 0;
+  const Seg x = seg_of<false>(a.sg, s, a.c.rows, a.c.ppr * PG);
+  return x.n > 0 ? (max(x.len, 0) + 31) / 32 : 0;
+}
+// Steps per split that cut all segments into equal pieces, `splits` of them and one more for each segment at most: the
+// launch has as many workgroups as run at once, and ragged rows keep them all equally long.
+__device__ __forceinline__ int even_steps(const AttendArgs& a, int lane) {
+  int total = 0;
+  for (int r = lane; r < a.sg.n_seg; r += 64) total += steps_of(a, r);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
+  return __builtin_amdgcn_readfirstlane(max((total + a.splits - 1) / a.splits, QCACHE_LEAST_STEPS));
+}
+
 template <int D, int QT, bool PAIR, bool KEYS, bool SEL>
 __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendArgs a) {
   constexpr int NS = D / 32, NJ = D / 16, CT = 16 * QT;
   const QCache& c = a.c;
   // block -> (split, column tile, head, segment[, token])
   int id = blockIdx.x;
-  int split, tile, h, s, tokn = 0;
-  if (a.by_xcd) {
+  int split, tile, h, s, tokn = 0, per = a.per;
+  if (KEYS && !SEL && a.even) {
+    const int lane = threadIdx.x & 63;
+    per = even_steps(a, lane);
+    h = id % c.H; id /= c.H;
+    tile = a.tiles - 1 - id % a.tiles; id /= a.tiles;
+    // piece `id` of the segments' pieces one after another
+    s = -1;
+    for (int r = 0, base = 0; r < a.sg.n_seg; r += 64) {
+      const int n = (steps_of(a, r + lane) + per - 1) / per;
+      int upto = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += y;
+      }
+      const uint64_t mine = __ballot(id - base < upto && id - base >= upto - n);
+      if (mine) {
+        const int j = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)mine) - 1);
+        s = r + j;
+        split = id - base - __builtin_amdgcn_readlane(upto - n, j);
+        break;
+      }
+      base += __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (s < 0) return;
+  } else if (a.by_xcd) {
     // Blocks go to the 8 XCDs in turn; those of one (segment, head) pair follow each other on one XCD and
     // read the same pages through its L2.  The tiles with the most positions go first.
     const int x = id & 7;
@@ -489,10 +533,9 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
   const int32_t* list = SEL ? a.sel + ((size_t)sg.t0 * c.H + h) * a.n_sel : nullptr;
   // (in KEYS mode every wave has the same columns; otherwise each stops at its own last position)
   const int steps = SEL ? 2 * a.n_sel : (vmax + 31) / 32;
-  // (every row in chunks of the same length, so that the workgroups with work take as long as each other; the
-  // last split takes what a row has beyond the estimate)
-  const int begin = split * a.per, inc = KEYS ? 4 : 1;
-  const int end = split == a.splits - 1 ? steps : min(steps, begin + a.per);
+  // (with `per` from an estimate of the length the last split takes what a row has beyond it)
+  const int begin = split * per, inc = KEYS ? 4 : 1;
+  const int end = split == a.splits - 1 && !a.even ? steps : min(steps, begin + per);
   // Lane j holds page, position and scales of the wave's j-th step from `from` on (a bit of `todo` each
   // where there is a page), so that no step waits for the page table: one round trip for 64 steps.
   int from = begin + (KEYS ? wave : 0), lane_page = 0, lane_pos = 0;
@@ -845,6 +888,11 @@ __global__ __launch_bounds__(256) void k_qcache_join(AttendArgs a) {
   if (tokn >= sg.n) return;
   const int tok = sg.t0 + tokn;
   const float* p = a.part + ((size_t)tok * heads + head) * a.splits * LD;
+  int splits = a.splits;
+  if (a.even) {
+    const int per = even_steps(a, lane);
+    splits = (steps_of(a, s) + per - 1) / per;
+  }
   // The first splits' sums are on their way before their factors are known: a launch of this size is all
   // latency.  Lane k holds the factor of split k0 + k.
   constexpr int PRE = 16;
@@ -852,22 +900,22 @@ __global__ __launch_bounds__(256) void k_qcache_join(AttendArgs a) {
 #pragma unroll
   for (int k = 0; k < PRE; ++k)
 #pragma unroll
-    for (int e = 0; e < E; ++e) pre[k][e] = p[(size_t)min(k, a.splits - 1) * LD + lane * E + e];
+    for (int e = 0; e < E; ++e) pre[k][e] = p[(size_t)max(min(k, splits - 1), 0) * LD + lane * E + e];
   float M = -INFINITY, L = 0.f, y[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) y[e] = 0.f;
-  for (int k = lane; k < a.splits; k += 64) M = fmaxf(M, p[(size_t)k * LD + D]);
+  for (int k = lane; k < splits; k += 64) M = fmaxf(M, p[(size_t)k * LD + D]);
   M = wave_max(M);
   auto factor = [](float f, int k) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), k)); };
-  for (int k0 = 0; k0 < a.splits; k0 += 64) {
+  for (int k0 = 0; k0 < splits; k0 += 64) {
     float f = 0.f, l = 0.f;
-    if (k0 + lane < a.splits) {
+    if (k0 + lane < splits) {
       const float* q = p + (size_t)(k0 + lane) * LD + D;
       f = q[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(q[0] - M);
       l = q[0] == -INFINITY ? 0.f : q[1] * f;
     }
     L += wave_sum(l);
-    const int n = min(a.splits - k0, 64);
+    const int n = min(splits - k0, 64);
     const float* q = p + (size_t)k0 * LD + lane * E;
     if (k0 == 0)
 #pragma unroll
@@ -1193,7 +1241,8 @@ hipError_t qcache_append(const QCache& c, const QSegs& sg, const void* k, int64_
 template <int D, bool PAIR>
 static hipError_t attend_launch(const QAttendPlan& p, AttendArgs& a, hipStream_t s) {
   const unsigned pairs = (unsigned)a.sg.n_seg * a.c.H;
-  const unsigned grid = (a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * p.tiles * p.splits * (a.sel ? a.sg.max_new : 1);
+  const unsigned grid = p.even ? a.c.H * p.tiles * (p.splits + a.sg.n_seg)
+                               : (a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * p.tiles * p.splits * (a.sel ? a.sg.max_new : 1);
   if (a.sel) k_qcache_attend<D, 1, PAIR, true, true><<<grid, 256, 0, s>>>(a);
   else if (!p.keys) k_qcache_attend<D, 2, PAIR, false, false><<<grid, 256, 0, s>>>(a);
   else if (p.qt == 1) k_qcache_attend<D, 1, PAIR, true, false><<<grid, 256, 0, s>>>(a);
@@ -1215,7 +1264,7 @@ hipError_t qcache_attend(const QCache& c, const QSegs& sg, const QAttendPlan& p,
   const bool shared = p.tiles > 1 || (sel && sg.max_new > 1);
   const int by_xcd = shared && (pairs % 8 == 0 || pairs >= 64);
   AttendArgs a{c, sg, q, ldq, o, ldo, (f16*)olo, dt, odt, aligned16(q, ldq, type_bytes(dt)),
-               aligned16(o, ldo, type_bytes(odt)), n_heads / c.H, scale, rope, sel, n_sel, p.tiles, p.splits, p.per, by_xcd, part};
+               aligned16(o, ldo, type_bytes(odt)), n_heads / c.H, scale, rope, sel, n_sel, p.tiles, p.splits, p.per, by_xcd, p.even, part};
   if (c.dh == 128) return pair ? attend_launch<128, true>(p, a, s) : attend_launch<128, false>(p, a, s);
   return pair ? attend_launch<64, true>(p, a, s) : attend_launch<64, false>(p, a, s);
 }

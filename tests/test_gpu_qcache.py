@@ -238,6 +238,20 @@ def test_long_row_in_many_splits(D, G, dtype):
     b.attend((130,), 1, dtype)
 
 
+@pytest.mark.parametrize("D,G,dtype", [(64, 1, "f16"), (128, 3, "f32")])
+def test_ragged_long_rows_in_even_pieces(D, G, dtype):
+    """Rows of very different lengths (and none), each cut into pieces of the same number of positions."""
+    lens = (2999, 5, 1500, 0, 700, 1, 64)
+    b = Both(len(lens), 47, 2, D, seed=G)
+    b.append(lens, "f16")
+    b.attend((1, 1, 1, 0, 1, 1, 1), G, dtype)
+    b.attend((0, 0, 9, 0, 3, 0, 0), G, dtype)
+    b.attend((1, 1, 1, 2, 1, 2, 1), G, dtype, max_len=3008)  # (row 3 and one token of row 5 see nothing)
+    many = Both(70, 24, 1, D, seed=7 + G)
+    many.append(tuple(1500 if r in (0, 63, 64, 69) else 1 + 7 * r % 90 for r in range(70)), "f16")
+    many.attend((1,) * 70, G, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("stride,shift", [(5, 0), (8, 3), (1, 1)])
 def test_strided_and_unaligned_queries_and_outputs(dtype, stride, shift):
