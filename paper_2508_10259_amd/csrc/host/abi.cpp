@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <string>
 #include <vector>
@@ -58,8 +59,22 @@ int current_device(int* dev, std::string& err) {
   return ams::S_OK;
 }
 
-// [p, p + bytes) must lie inside one device allocation of `dev`.
-bool dev_range(const void* p, size_t bytes, int dev, const char* what, std::string& err) {
+// The same for the calls that a decode step makes for every layer: a device once found to be a gfx950 is not
+// asked again.
+int current_device_again(int* dev, std::string& err) {
+  static std::atomic<uint64_t> known{0};
+  if (hipGetDevice(dev) == hipSuccess && *dev >= 0 && *dev < 64 && (known.load(std::memory_order_relaxed) >> *dev & 1))
+    return ams::S_OK;
+  (void)hipGetLastError();
+  const int s = current_device(dev, err);
+  if (s == ams::S_OK && *dev < 64) known.fetch_or((uint64_t)1 << *dev, std::memory_order_relaxed);
+  return s;
+}
+
+// [p, p + bytes) must lie inside one device allocation of `dev`; its first and last byte + 1 go to *lo and *hi
+// when given.
+bool dev_range(const void* p, size_t bytes, int dev, const char* what, std::string& err, const char** lo = nullptr,
+               const char** hi = nullptr) {
   if (!p) {
     err = std::string(what) + " is NULL";
     return false;
@@ -81,8 +96,27 @@ bool dev_range(const void* p, size_t bytes, int dev, const char* what, std::stri
     err = std::string(what) + " is smaller than " + std::to_string(bytes) + " bytes";
     return false;
   }
+  if (lo) *lo = (const char*)base;
+  if (hi) *hi = (const char*)base + size;
   return true;
 }
+
+// dev_range of several arrays of one call: those that lie in an allocation found for an earlier one of them (an
+// allocator hands out parts of large ones) are not looked up again.  Nothing outlives the call.
+struct DevRanges {
+  int dev;
+  int n = 0;
+  const char *lo[8], *hi[8];
+  bool operator()(const void* p, size_t bytes, const char* what, std::string& err) {
+    const char* c = (const char*)p;
+    for (int i = 0; i < n; ++i)
+      if (c >= lo[i] && c < hi[i] && bytes <= (size_t)(hi[i] - c)) return true;
+    if (n == 8) return dev_range(p, bytes, dev, what, err);
+    if (!dev_range(p, bytes, dev, what, err, &lo[n], &hi[n])) return false;
+    ++n;
+    return true;
+  }
+};
 
 // Workgroups of one launch of the 8-bit cache's kernels (of 1,024 threads at most: a grid has fewer than
 // 2^32 threads).
@@ -502,8 +536,8 @@ bool qcache_type(int32_t dtype, std::string& e) {
 }
 
 // A [n_tok][heads][head_dim] tensor with a token stride of ld elements.
-bool qcache_tensor(const void* p, int64_t ld, int32_t n_tok, int64_t width, int32_t dtype, int dev, const char* what,
-                   std::string& e) {
+bool qcache_tensor(const void* p, int64_t ld, int32_t n_tok, int64_t width, int32_t dtype, DevRanges& in,
+                   const char* what, std::string& e) {
   const int64_t es = dtype == AMS_F32 ? 4 : 2;
   if (ld < width || ld > ((int64_t)1 << 40)) {
     e = std::string(what) + ": token stride must be at least heads * head_dim (and at most 2^40) elements";
@@ -513,10 +547,10 @@ bool qcache_tensor(const void* p, int64_t ld, int32_t n_tok, int64_t width, int3
     e = std::string(what) + " is not aligned to its type";
     return false;
   }
-  return dev_range(p, (size_t)(((int64_t)(n_tok - 1) * ld + width) * es), dev, what, e);
+  return in(p, (size_t)(((int64_t)(n_tok - 1) * ld + width) * es), what, e);
 }
 
-bool qcache_arrays(const ams_qcache* c, const int32_t* tok_off, const int32_t* kv_len, int dev, std::string& e) {
+bool qcache_arrays(const ams_qcache* c, const int32_t* tok_off, const int32_t* kv_len, DevRanges& in, std::string& e) {
   const void* p[] = {c->k, c->v, c->k_scale, c->v_scale, c->k_bounds};
   for (const void* x : p)
     if ((uintptr_t)x & 15) {
@@ -528,12 +562,12 @@ bool qcache_arrays(const ams_qcache* c, const int32_t* tok_off, const int32_t* k
     return false;
   }
   const size_t ph = (size_t)c->n_pages * c->n_kv_heads, d = c->head_dim;
-  return dev_range(c->k, ph * 64 * d, dev, "cache k", e) && dev_range(c->v, ph * 64 * d, dev, "cache v", e) &&
-         dev_range(c->k_scale, ph * 4, dev, "cache k_scale", e) && dev_range(c->v_scale, ph * 4, dev, "cache v_scale", e) &&
-         dev_range(c->k_bounds, ph * 2 * d, dev, "cache k_bounds", e) &&
-         dev_range(c->page_table, (size_t)c->rows * c->pages_per_row * 4, dev, "cache page_table", e) &&
-         dev_range(tok_off, ((size_t)c->rows + 1) * 4, dev, "tok_off", e) &&
-         dev_range(kv_len, (size_t)c->rows * 4, dev, "kv_len", e);
+  return in(c->k, ph * 64 * d, "cache k", e) && in(c->v, ph * 64 * d, "cache v", e) &&
+         in(c->k_scale, ph * 4, "cache k_scale", e) && in(c->v_scale, ph * 4, "cache v_scale", e) &&
+         in(c->k_bounds, ph * 2 * d, "cache k_bounds", e) &&
+         in(c->page_table, (size_t)c->rows * c->pages_per_row * 4, "cache page_table", e) &&
+         in(tok_off, ((size_t)c->rows + 1) * 4, "tok_off", e) &&
+         in(kv_len, (size_t)c->rows * 4, "kv_len", e);
 }
 
 ams::QCache qcache_view(const ams_qcache* c) {
@@ -561,11 +595,11 @@ ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, co
   max_new = std::min(max_new, n_tok);
   if (((int64_t)(max_new + 62) / 64 + 1) * cache->n_kv_heads * cache->rows > QCACHE_MAX_BLOCKS)
     return fail(AMS_EINVAL, "too many pages for one call: rows * n_kv_heads * max_new / 64 is above 2^22");
-  int dev = 0;
-  if (int s = current_device(&dev, e)) return fail(s, e);
+  DevRanges in{0};
+  if (int s = current_device_again(&in.dev, e)) return fail(s, e);
   const int64_t width = (int64_t)cache->n_kv_heads * cache->head_dim;
-  if (!qcache_arrays(cache, tok_off, kv_len, dev, e) || !qcache_tensor(k, ldk, n_tok, width, dtype, dev, "k", e) ||
-      !qcache_tensor(v, ldv, n_tok, width, dtype, dev, "v", e))
+  if (!qcache_arrays(cache, tok_off, kv_len, in, e) || !qcache_tensor(k, ldk, n_tok, width, dtype, in, "k", e) ||
+      !qcache_tensor(v, ldv, n_tok, width, dtype, in, "v", e))
     return fail(AMS_EINVAL, e);
   const ams::QSegs sg{nullptr, tok_off, nullptr, kv_len, 0, cache->rows, n_tok, max_new};
   hipError_t r = ams::qcache_append(qcache_view(cache), sg, k, ldk, v, ldv, dtype, nullptr, (hipStream_t)stream);
@@ -604,12 +638,12 @@ ams_status ams_qcache_attend(const ams_qcache* cache, const int32_t* tok_off, co
   if ((uintptr_t)ws & 15) return fail(AMS_EINVAL, "ws must be 16-byte aligned");
   if (ws_bytes < need) return fail(AMS_ENOMEM, "workspace too small: need " + std::to_string(need));
   if ((uintptr_t)selected & 3) return fail(AMS_EINVAL, "selected must be 4-byte aligned");
-  int dev = 0;
-  if (int s = current_device(&dev, e)) return fail(s, e);
+  DevRanges in{0};
+  if (int s = current_device_again(&in.dev, e)) return fail(s, e);
   const int64_t width = (int64_t)n_heads * cache->head_dim;
-  if (!qcache_arrays(cache, tok_off, kv_len, dev, e) || !qcache_tensor(q, ldq, n_tok, width, dtype, dev, "q", e) ||
-      !qcache_tensor(out, ldo, n_tok, width, dtype, dev, "out", e) ||
-      (need && !dev_range(ws, need, dev, "ws", e)) || (selected && !dev_range(selected, list, dev, "selected", e)))
+  if (!qcache_arrays(cache, tok_off, kv_len, in, e) || !qcache_tensor(q, ldq, n_tok, width, dtype, in, "q", e) ||
+      !qcache_tensor(out, ldo, n_tok, width, dtype, in, "out", e) ||
+      (need && !in(ws, need, "ws", e)) || (selected && !in(selected, list, "selected", e)))
     return fail(AMS_EINVAL, e);
   const ams::QCache c = qcache_view(cache);
   const ams::QSegs sg{nullptr, tok_off, nullptr, kv_len, 0, cache->rows, n_tok, max_new};

@@ -14,6 +14,7 @@
 //     tile 0, then of tile 1: one dword of the value page each, and the lane's own scores.
 // A scale is a power of two: e4m3 keeps its three mantissa bits at any exponent, so a finer scale
 // would not round better, and moving a page to a larger scale is exact but for subnormals.
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -943,7 +944,7 @@ __global__ __launch_bounds__(256) void k_qcache_join(AttendArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Selection.  A workgroup per (token, KV head).  The score of a page is an upper bound of q . k over
+// Selection.  A workgroup per KV head and token, or 16 / G of a row's tokens (they read the same bounds).  The score of a page is an upper bound of q . k over
 // its keys, from each channel's largest and smallest key, in whole numbers (|q^| <= 127 times bounds of
 // at most 112, 128 channels: below 2^21), so it has the same bits in any order of summation:
 //   2^ke max over heads of sum_d max(q^_d, 0) hi_d + min(q^_d, 0) lo_d
@@ -956,7 +957,7 @@ struct SelectArgs {
   QSegs sg;
   const void* q;
   int64_t ldq;
-  int dt, alq, G, n_sel;
+  int dt, alq, G, n_sel, toks;  // toks: tokens of a row that a workgroup takes
   const float2* rope;
   int32_t* sel;
 };
@@ -964,7 +965,7 @@ struct SelectArgs {
 constexpr int SEL_OUT = 0;  // the key of a page that cannot be chosen; every other key is larger
 
 // The n_sel best of np <= 64 N keys by one wave, N keys to a lane: the key of rank n_sel bit by bit, counts in the
-// scalar unit .
+// scalar unit.
 template <int N>
 __device__ __forceinline__ void select_wave(const uint32_t* key, int np, int n_sel, int lane, int32_t* out) {
   uint32_t k[N], T = 0u;
@@ -995,10 +996,24 @@ __device__ __forceinline__ void select_wave(const uint32_t* key, int np, int n_s
   for (int p = at + lane; p < n_sel; p += 64) out[p] = -1;
 }
 
+// Every page in view of a token that sees n_sel or fewer: the ones in the pool, in order.
+__device__ __forceinline__ void select_all(const QCache& c, int row, int np, int n_sel, int lane, int32_t* out) {
+  int at = 0;
+  for (int p0 = 0; p0 < np; p0 += 64) {
+    const int p = p0 + lane;
+    const bool ok = p < np && (unsigned)c.pt[(size_t)row * c.ppr + p] < (unsigned)c.n_pages;
+    const uint64_t b = __ballot(ok);
+    if (ok) out[at + (int)__popcll(b & ((1ull << lane) - 1ull))] = p;
+    at += (int)__popcll(b);
+  }
+  for (int p = at + lane; p < n_sel; p += 64) out[p] = -1;
+}
+
 template <int D, int NT>
 __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
-  constexpr int NW = NT / 64, NB = 2 * D / 64, U = 4;
-  extern __shared__ uint32_t key[];  // [ppr]
+  // U groups of 16 pages at a time: a wave waits twice (page table, bounds) for all of them
+  constexpr int NW = NT / 64, NB = 2 * D / 64, U = NT == 256 ? 4 : 8;
+  extern __shared__ uint32_t key[];  // [tokens][ppr]
   __shared__ uint32_t hist[256];
   __shared__ uint32_t pick[2];
   __shared__ uint32_t wsum[2][NW];
@@ -1006,39 +1021,52 @@ __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
   int id = blockIdx.x;
   const int h = id % c.H;
   id /= c.H;
-  const int tokn = id % a.sg.max_new, s = id / a.sg.max_new;
+  const int per_row = (a.sg.max_new + a.toks - 1) / a.toks;
+  const int tok0 = id % per_row * a.toks, s = id / per_row;
   const Seg sg = seg_of(a.sg, s, c.rows, c.ppr * PG);
-  if (tokn >= sg.n) return;
+  if (tok0 >= sg.n) return;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int tok = sg.t0 + tokn, vis = max(sg.p0 + tokn + 1, 0), np = (vis + PG - 1) / PG, G = a.G;
-  int32_t* out = a.sel + ((size_t)tok * c.H + h) * a.n_sel;
+  // nt tokens; token t sees `vis_of(t)` positions on `pages_of(t)` pages, the last one the most
+  const int nt = min(a.toks, sg.n - tok0), G = a.G;
+  auto vis_of = [&](int t) { return max(sg.p0 + tok0 + t + 1, 0); };
+  auto pages_of = [&](int t) { return (vis_of(t) + PG - 1) / PG; };
+  auto out_of = [&](int t) { return a.sel + ((size_t)(sg.t0 + tok0 + t) * c.H + h) * a.n_sel; };
+  const int np = pages_of(nt - 1);
 
   if (np > a.n_sel) {
-    // U groups of 16 pages at a time, so that a wave waits twice (page table, bounds) and not twice for each;
-    // the first ones are on their way while the queries are
     int page[U];
     float ks[U];
     i32x4 bound[U][NB];
-    auto fetch = [&](int p0) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) page[u] = c.pt[(size_t)sg.row * c.ppr + min(p0 + u * NW * 16 + i, np - 1)];
+    auto fetch_pages = [&](int p0) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const bool ok = (unsigned)page[u] < (unsigned)c.n_pages;
-        const size_t ph = (size_t)(ok ? page[u] : 0) * c.H + h;
+        page[u] = c.pt[(size_t)sg.row * c.ppr + min(p0 + u * NW * 16 + i, np - 1)];
+        page[u] = (unsigned)page[u] < (unsigned)c.n_pages ? page[u] : -1;
+      }
+    };
+    auto fetch = [&](auto from, auto to) {
+#pragma unroll
+      for (int u = decltype(from)::value; u < decltype(to)::value; ++u) {
+        const size_t ph = (size_t)max(page[u], 0) * c.H + h;
         const i32x4* b = (const i32x4*)(c.kb + ph * (2 * D)) + g;
-        page[u] = ok ? page[u] : -1;
         ks[u] = c.ks[ph];
 #pragma unroll
         for (int n = 0; n < NB; ++n) bound[u][n] = b[4 * n];
       }
     };
-    fetch(wave * 16);
-    // the largest |q| of the group's heads; lane (i, g) reads head i's channels 64 b + 16 g .. of each
-    // block b of 64 (all waves the same)
+    constexpr std::integral_constant<int, 0> NONE{};
+    constexpr std::integral_constant<int, 4> SOME{};
+    constexpr std::integral_constant<int, U> ALL{};
+    fetch_pages(wave * 16);  // on their way while the queries are (as many as the registers hold beside those)
+    fetch(NONE, SOME);
+    // Row i of the products: one token's head c0 + i, or, of several tokens, head i % G of token i / G.  Lane (i, g)
+    // reads its channels 64 b + 16 g .. of each block b of 64 (all waves the same).
+    const int rt = a.toks == 1 ? 0 : i / G;
+    const bool live = rt < nt;
+    const int vis = live ? vis_of(rt) : 0;
     auto load16 = [&](int col, int b, float* x) {
-      const int64_t at = (int64_t)tok * a.ldq + (int64_t)(h * G + col) * D + (64 * b + 16 * g) % D;
+      const int64_t at = (int64_t)(sg.t0 + tok0 + rt) * a.ldq + (int64_t)(h * G + col) * D + (64 * b + 16 * g) % D;
       load8(a.q, at, a.dt, a.alq, x);
       load8(a.q, at + 8, a.dt, a.alq, x + 8);
       if (a.rope) {
@@ -1056,26 +1084,31 @@ __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
         }
       }
     };
+    const int first_col = a.toks == 1 ? i : i % G;
+    // the largest |q| of the group's heads
     float m = 0.f;
-    for (int col = i; col < G; col += 16)
+    if (live)
+      for (int col = first_col; col < G; col += 16)
 #pragma unroll
-      for (int b = 0; b < D / 64; ++b) {
-        float x[16];
-        load16(col, b, x);
+        for (int b = 0; b < D / 64; ++b) {
+          float x[16];
+          load16(col, b, x);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[e]));
-      }
-    m = wave_max(m);
+          for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[e]));
+        }
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    for (int o = 1; o < (a.toks == 1 ? 16 : G); o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     int ex;
     frexpf(m, &ex);
     const bool flat = !(m > 0.f) || m == INFINITY;  // nothing to rank by: every score 0
     for (int c0 = 0; c0 < G; c0 += 16) {
-      const int col = c0 + i;
-      i32x4 B[NB];
+      const int col = c0 + first_col;
+      i32x4 A[NB];
 #pragma unroll
       for (int b = 0; b < D / 64; ++b) {
         float x[16];
-        if (col < G && !flat) load16(col, b, x);
+        if (live && col < G && !flat) load16(col, b, x);
         else
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[e] = 0.f;
@@ -1087,42 +1120,66 @@ __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
           up[e / 4] |= (max(v, 0) & 255) << (8 * (e % 4));
           dn[e / 4] |= (min(v, 0) & 255) << (8 * (e % 4));
         }
-        B[b] = up;
-        B[b + D / 64] = dn;
+        A[b] = up;
+        A[b + D / 64] = dn;
       }
-      // heads as rows, pages as columns: a lane's sums are those of its page
       for (int p0 = wave * 16; p0 < np; p0 += NW * 16 * U) {
-        if (c0 > 0 || p0 != wave * 16) fetch(p0);
+        const bool begun = c0 == 0 && p0 == wave * 16;
+        if (!begun) {
+          fetch_pages(p0);
+          fetch(NONE, SOME);
+        }
+        fetch(SOME, ALL);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-          for (int n = 0; n < NB; ++n) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(B[n], bound[u][n], acc, 0, 0, 0);
-          int v = INT_MIN;
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (c0 + 4 * g + r < G) v = max(v, acc[r]);
-          v = max(v, __shfl_xor(v, 16, 64));
-          v = max(v, __shfl_xor(v, 32, 64));
-          const int lp = p0 + u * NW * 16 + i;
-          if (g == 0 && lp < np) {
+          for (int n = 0; n < NB; ++n) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(A[n], bound[u][n], acc, 0, 0, 0);
+          const int lp = p0 + u * NW * 16 + i;  // the lane's page; its rows are 4 g + r
+          auto put = [&](int t, int v) {
+            if (t >= nt || lp >= np) return;
             uint32_t k = __float_as_uint((float)v * ks[u]);
             k = k & 0x80000000u ? ~k : k | 0x80000000u;
-            if (lp == np - 1) k = 0xFFFFFFFFu;
+            if (lp == pages_of(t) - 1) k = 0xFFFFFFFFu;
             if (page[u] < 0) k = SEL_OUT;
-            key[lp] = c0 ? max(key[lp], k) : k;
+            uint32_t* at = key + (size_t)t * c.ppr + lp;
+            *at = c0 ? max(*at, k) : k;
+          };
+          if (a.toks == 1) {
+            int v = INT_MIN;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (c0 + 4 * g + r < G) v = max(v, acc[r]);
+            v = max(v, __shfl_xor(v, 16, 64));
+            v = max(v, __shfl_xor(v, 32, 64));
+            if (g == 0) put(0, v);
+          } else if (G == 1) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) put(4 * g + r, acc[r]);
+          } else if (G == 2) {
+            put(2 * g, max(acc[0], acc[1]));
+            put(2 * g + 1, max(acc[2], acc[3]));
+          } else {
+            int v = max(max(acc[0], acc[1]), max(acc[2], acc[3]));
+            if (G == 8) v = max(v, __shfl_xor(v, 16, 64));
+            if (G == 4 || (g & 1) == 0) put(4 * g / G, v);
           }
         }
       }
     }
     __syncthreads();
-    if (np <= 1024) {
-      if (wave) return;
-      if (np <= 64) select_wave<1>(key, np, a.n_sel, lane, out);
-      else if (np <= 256) select_wave<4>(key, np, a.n_sel, lane, out);
-      else select_wave<16>(key, np, a.n_sel, lane, out);
+    if (c.ppr <= 1024) {
+      for (int t = wave; t < nt; t += NW) {
+        const int n = pages_of(t);
+        const uint32_t* k = key + (size_t)t * c.ppr;
+        if (n <= a.n_sel) select_all(c, sg.row, n, a.n_sel, lane, out_of(t));
+        else if (n <= 64) select_wave<1>(k, n, a.n_sel, lane, out_of(t));
+        else if (n <= 256) select_wave<4>(k, n, a.n_sel, lane, out_of(t));
+        else select_wave<16>(k, n, a.n_sel, lane, out_of(t));
+      }
       return;
     }
+    int32_t* out = out_of(0);  // (one token)
     // the key of rank n_sel: digit by digit, `need` of the keys with the digits so far are wanted
     uint32_t prefix = 0u, need = a.n_sel;
     for (int d = 24; d >= 0; d -= 8) {
@@ -1201,18 +1258,7 @@ __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
     }
     return;
   }
-  // every page in view: the ones in the pool, in order
-  if (wave == 0) {
-    int at = 0;
-    for (int p0 = 0; p0 < np; p0 += 64) {
-      const int p = p0 + lane;
-      const bool ok = p < np && (unsigned)c.pt[(size_t)sg.row * c.ppr + p] < (unsigned)c.n_pages;
-      const uint64_t b = __ballot(ok);
-      if (ok) out[at + __popcll(b & ((1ull << lane) - 1ull))] = p;
-      at += __popcll(b);
-    }
-    for (int p = at + lane; p < a.n_sel; p += 64) out[p] = -1;
-  }
+  for (int t = wave; t < nt; t += NW) select_all(c, sg.row, pages_of(t), a.n_sel, lane, out_of(t));
 }
 
 bool aligned16(const void* p, int64_t ld, int es) { return ((uintptr_t)p & 15) == 0 && (ld * es) % 16 == 0; }
@@ -1270,8 +1316,9 @@ hipError_t qcache_attend(const QCache& c, const QSegs& sg, const QAttendPlan& p,
 }
 
 template <int D, int NT>
-static hipError_t select_launch(const SelectArgs& a, unsigned grid, hipStream_t s) {
-  const size_t lds = (size_t)a.c.ppr * 4;
+static hipError_t select_launch(const SelectArgs& a, hipStream_t s) {
+  const unsigned grid = (unsigned)a.sg.n_seg * a.c.H * ((a.sg.max_new + a.toks - 1) / a.toks);
+  const size_t lds = (size_t)a.toks * a.c.ppr * 4;
   if (lds > 60 * 1024) {  // above 64 KB with the kernel's own
     hipError_t e = hipFuncSetAttribute((const void*)k_qcache_select<D, NT>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)lds);
@@ -1283,11 +1330,12 @@ static hipError_t select_launch(const SelectArgs& a, unsigned grid, hipStream_t 
 
 hipError_t qcache_select(const QCache& c, const QSegs& sg, int n_heads, const void* q, int64_t ldq,
                          int dt, const float2* rope, int n_sel, int32_t* sel, hipStream_t s) {
-  SelectArgs a{c, sg, q, ldq, dt, aligned16(q, ldq, type_bytes(dt)), n_heads / c.H, n_sel, rope, sel};
-  const unsigned grid = (unsigned)sg.n_seg * c.H * sg.max_new;
-  if (c.ppr <= 256)
-    return c.dh == 128 ? select_launch<128, 256>(a, grid, s) : select_launch<64, 256>(a, grid, s);
-  return c.dh == 128 ? select_launch<128, 512>(a, grid, s) : select_launch<64, 512>(a, grid, s);
+  SelectArgs a{c, sg, q, ldq, dt, aligned16(q, ldq, type_bytes(dt)), n_heads / c.H, n_sel, 1, rope, sel};
+  // the rows of one product hold the heads of several tokens where they divide it; their keys fit 48 KB of LDS
+  if (a.G == 1 || a.G == 2 || a.G == 4 || a.G == 8)
+    if (c.ppr <= 1024) a.toks = std::max(1, std::min({16 / a.G, 12288 / c.ppr, sg.max_new}));
+  if (c.ppr <= 256) return c.dh == 128 ? select_launch<128, 256>(a, s) : select_launch<64, 256>(a, s);
+  return c.dh == 128 ? select_launch<128, 512>(a, s) : select_launch<64, 512>(a, s);
 }
 
 }  // namespace ams
