@@ -84,11 +84,7 @@ def append(c: Cache, row: int, p0: int, k: np.ndarray, v: np.ndarray) -> None:
             for which, z in (("k", x), ("v", y)):
                 codes = c.k[page, h] if which == "k" else c.v[page, h].transpose(0, 2, 1).reshape(PAGE, D).copy()
                 es = c.ke if which == "k" else c.ve
-                # (a token's overwritten channel 0 still counts towards the scale)
                 amax = float(np.max(np.abs(np.where(np.isnan(z), 0.0, z)))) if z.size else 0.0
-                if which == "k":
-                    raw = k[a - p0:b - p0, h].astype(np.float64)
-                    amax = float(np.max(np.abs(np.where(np.isnan(raw), 0.0, np.clip(raw, -SAT, SAT)))))
                 e = scale_exponent(amax)
                 shift = 0
                 if s0 > 0:

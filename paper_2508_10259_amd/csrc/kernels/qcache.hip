@@ -166,8 +166,9 @@ __device__ __forceinline__ uint32_t rescale_codes(uint32_t w, int de) {
 
 // ---------------------------------------------------------------------------
 // Append.  One workgroup per (page, head): it alone writes that page's codes, scales and bounds.
-// D/8 lanes take a token (8 channels each), a workgroup NT / (D/8) tokens at a time.  The tokens
-// stay in registers from the maximum, which sets the scale, to the rounding.
+// D/8 lanes take a quad of slots, 8 channels each: a lane's four values of a channel are one dword of the value page,
+// its four keys 8 bytes of their rows.  With few tokens they take one slot, and a value is a byte of that dword.  The tokens stay in registers from the maximum, which sets the scale, to the
+// rounding.
 
 // The least e >= -32 with a <= 448 2^e (448 = 0.875 * 2^9).
 __device__ __forceinline__ int scale_exponent(float a) {
@@ -191,9 +192,9 @@ struct AppendArgs {
   const float2* rope;
 };
 
-template <int D, int NT, int PASSES>
+template <int D, int NT, int PER>  // PER: slots of a lane
 __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
-  constexpr int LPT = D / 8, TPP = NT / LPT, NW = NT / 64;
+  constexpr int LPT = D / 8, NW = NT / 64;
   const QCache& c = a.c;
   const int h = blockIdx.x % c.H, rest = blockIdx.x / c.H, chunk = rest % a.chunks, s = rest / a.chunks;
   const Seg sg = seg_of(a.sg, s, c.rows, c.ppr * PG);
@@ -201,60 +202,106 @@ __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
   if (sg.n <= 0 || sg.len <= first) return;
   const int lp = first / PG + chunk;
   if (lp * PG >= sg.len) return;
-  const int page = page_of(c, sg.row, lp);
-  if (page < 0) return;
-  const int s0 = max(first - lp * PG, 0), s1 = min(sg.len - lp * PG, PG), cnt = s1 - s0;
-  const int tok = sg.t0 + (lp * PG + s0 - sg.p0);  // token at slot s0
+  const int page = page_of(c, sg.row, lp);  // (looked at after the tokens' loads, which do not wait for it)
+  const int s0 = max(first - lp * PG, 0), s1 = min(sg.len - lp * PG, PG);
+  const int tok = sg.t0 + (lp * PG - sg.p0);  // token at slot 0 (slots s0 .. s1 - 1 are this call's)
   const int tid = threadIdx.x, sub = tid % LPT, grp = tid / LPT, lane = tid & 63, wave = tid >> 6;
+  const int slot0 = PER == 4 ? grp * 4 : s0 + grp;
   __shared__ float red[2][NW];
-  __shared__ __align__(16) uint8_t vt[PASSES * TPP][D];
   __shared__ float bred[2][NW][D];
 
-  float k[PASSES][8], v[PASSES][8];
-  float ka = 0.f, va = 0.f;
+  float k[PER][8], v[PER][8];
+  uint32_t fresh = 0u;  // a byte for each of the lane's slots that this call writes
 #pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    const int i = p * TPP + grp;
-    if (i < cnt) {
-      load8(a.k, (int64_t)(tok + i) * a.ldk + (int64_t)h * D + sub * 8, a.dt, a.alk, k[p]);
-      load8(a.v, (int64_t)(tok + i) * a.ldv + (int64_t)h * D + sub * 8, a.dt, a.alv, v[p]);
+  for (int p = 0; p < PER; ++p) {
+    const int slot = slot0 + p;
+    if (slot >= s0 && slot < s1) {
+      load8(a.k, (int64_t)(tok + slot) * a.ldk + (int64_t)h * D + sub * 8, a.dt, a.alk, k[p]);
+      load8(a.v, (int64_t)(tok + slot) * a.ldv + (int64_t)h * D + sub * 8, a.dt, a.alv, v[p]);
+      fresh |= 0xFFu << (8 * p);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) k[p][e] = v[p][e] = 0.f;
     }
+  }
+  if (page < 0) return;
+  // each channel's largest and smallest key (rounding keeps their order, so their codes are the codes' bounds), and
+  // the largest |value|
+  float hi[8], lo[8], va = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    hi[e] = -INFINITY;
+    lo[e] = INFINITY;
+  }
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
     if (a.rope) {  // pair (i, i + D/2): the partner's channels sit D/16 lanes away
-      const float2* tab = a.rope + (size_t)min(lp * PG + s0 + i, c.ppr * PG - 1) * (D / 2) + (sub % (LPT / 2)) * 8;
+      const float2* tab =
+          a.rope + (size_t)min(lp * PG + slot0 + p, c.ppr * PG - 1) * (D / 2) + (sub % (LPT / 2)) * 8;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float other = __shfl_xor(k[p][e], LPT / 2, 64);
         const float2 cs = tab[e];
-        float lo, hi;
+        float x, y;
         const bool low = sub < LPT / 2;
-        rope_pair(low ? k[p][e] : other, low ? other : k[p][e], cs.x, cs.y, lo, hi);
-        k[p][e] = low ? lo : hi;
+        rope_pair(low ? k[p][e] : other, low ? other : k[p][e], cs.x, cs.y, x, y);
+        k[p][e] = low ? x : y;
       }
     }
     bool nan = false;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      nan |= k[p][e] != k[p][e] || v[p][e] != v[p][e];
-      if (k[p][e] == k[p][e]) k[p][e] = fminf(fmaxf(k[p][e], -F16_MAX), F16_MAX);
-      v[p][e] = v[p][e] == v[p][e] ? fminf(fmaxf(v[p][e], -F16_MAX), F16_MAX) : 0.f;
-      ka = fmaxf(ka, fabsf(k[p][e]));
-      va = fmaxf(va, fabsf(v[p][e]));
+    for (int e = 0; e < 8; ++e) nan |= __builtin_isunordered(k[p][e], v[p][e]);
+    const uint64_t nans = __ballot(nan);
+    if (nans) {
+      // a NaN anywhere in the token's key or value: its key gets one, its value none, so that the
+      // queries which see the token read NaN and no other query does (0 * NaN would reach those)
+      const bool mine = nans >> (lane - lane % LPT) & ((1ull << LPT) - 1ull);
+      if (mine && sub == 0) k[p][0] = __uint_as_float(0x7FC00000u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (k[p][e] == k[p][e]) k[p][e] = fminf(fmaxf(k[p][e], -F16_MAX), F16_MAX);
+        v[p][e] = v[p][e] == v[p][e] ? fminf(fmaxf(v[p][e], -F16_MAX), F16_MAX) : 0.f;
+      }
+    } else {  // one instruction each
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        k[p][e] = __builtin_amdgcn_fmed3f(k[p][e], -F16_MAX, F16_MAX);
+        v[p][e] = __builtin_amdgcn_fmed3f(v[p][e], -F16_MAX, F16_MAX);
+      }
     }
-    // a NaN anywhere in the token's key or value: its key gets one, its value none, so that the
-    // queries which see the token read NaN and no other query does (0 * NaN would reach those)
-    const uint64_t nans = __ballot(nan) >> (lane - lane % LPT);
-    if (sub == 0 && (nans & ((1ull << LPT) - 1ull))) k[p][0] = __uint_as_float(0x7FC00000u);
+    if (fresh >> (8 * p) & 1u) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {  // (a NaN counts in none)
+        hi[e] = fmaxf(hi[e], k[p][e]);
+        lo[e] = fminf(lo[e], k[p][e]);
+        va = fmaxf(va, fabsf(v[p][e]));
+      }
+    }
   }
+  float ka = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ka = fmaxf(ka, fmaxf(hi[e], -lo[e]));
   ka = wave_max(ka);
   va = wave_max(va);
+  // the channels' bounds over the wave's tokens, then over the workgroup's
+#pragma unroll
+  for (int o = LPT; o < 64; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      hi[e] = fmaxf(hi[e], __shfl_xor(hi[e], o, 64));
+      lo[e] = fminf(lo[e], __shfl_xor(lo[e], o, 64));
+    }
   if (NW > 1) {
     if (lane == 0) {
       red[0][wave] = ka;
       red[1][wave] = va;
     }
+    if (lane < LPT)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        bred[0][wave][sub * 8 + e] = hi[e];
+        bred[1][wave][sub * 8 + e] = lo[e];
+      }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
@@ -273,60 +320,61 @@ __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
   }
 
   uint8_t* kpage = c.k + ph * (PG * D);
-  uint32_t* vpage = (uint32_t*)(c.v + ph * (PG * D));
-  if (kd < 0) {
+  uint8_t* vpage = c.v + ph * (PG * D);
+  if (kd < 0)
     for (int i = tid; i < s0 * (D / 8); i += NT) {
       uint2* w = (uint2*)kpage + i;
       const uint2 x = *w;
       *w = uint2{rescale_codes(x.x, kd), rescale_codes(x.y, kd)};
     }
+  if (vd < 0) {
+    // (PER 4: the quad that holds older and new slots is left to its lanes)
+    const int quads = PER == 4 ? s0 / 4 : (s0 + 3) / 4;
+    for (int i = tid; i < quads * D; i += NT) {
+      uint32_t* w = (uint32_t*)vpage + i;
+      const int n = s0 - i / D * 4;
+      const uint32_t older = n >= 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
+      *w = (rescale_codes(*w, vd) & older) | (*w & ~older);
+    }
+    if (PER == 1) __syncthreads();
   }
-  float hi[8], lo[8];
+  const float ki = ldexpf(1.f, -ke), vi = ldexpf(1.f, -ve);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    hi[e] = -INFINITY;
-    lo[e] = INFINITY;
-  }
-#pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    const int i = p * TPP + grp;
-    if (i < cnt) {
+  for (int p = 0; p < PER; ++p)
+    if (fresh >> (8 * p) & 1u) {
       uint2 w;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) k[p][e] = ldexpf(k[p][e], -ke);
-      w.x = pack_codes(k[p][0], k[p][1], k[p][2], k[p][3]);
-      w.y = pack_codes(k[p][4], k[p][5], k[p][6], k[p][7]);
-      *(uint2*)(kpage + (s0 + i) * D + sub * 8) = w;
-      float x[8];
-      unpack_codes(w.x, x);
-      unpack_codes(w.y, x + 4);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {  // (a NaN code counts in no bound)
-        hi[e] = fmaxf(hi[e], x[e]);
-        lo[e] = fminf(lo[e], x[e]);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[p][e] = ldexpf(v[p][e], -ve);
-      w.x = pack_codes(v[p][0], v[p][1], v[p][2], v[p][3]);
-      w.y = pack_codes(v[p][4], v[p][5], v[p][6], v[p][7]);
-      *(uint2*)(&vt[i][sub * 8]) = w;
+      w.x = pack_codes(k[p][0] * ki, k[p][1] * ki, k[p][2] * ki, k[p][3] * ki);
+      w.y = pack_codes(k[p][4] * ki, k[p][5] * ki, k[p][6] * ki, k[p][7] * ki);
+      *(uint2*)(kpage + (slot0 + p) * D + sub * 8) = w;
     }
+  uint8_t* vdst = vpage + ((slot0 >> 2) * D + sub * 8) * 4;  // eight channels of the quad: 32 bytes
+  if (PER == 1 && fresh) {  // a byte of each dword
+    const uint32_t w[2] = {pack_codes(v[0][0] * vi, v[0][1] * vi, v[0][2] * vi, v[0][3] * vi),
+                           pack_codes(v[0][4] * vi, v[0][5] * vi, v[0][6] * vi, v[0][7] * vi)};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) vdst[4 * e + (slot0 & 3)] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
   }
-  // the channels' bounds over the workgroup's tokens
+  if (PER == 4 && fresh) {
+    uint32_t w[8];
 #pragma unroll
-  for (int o = LPT; o < 64; o <<= 1)
+    for (int e = 0; e < 8; ++e)
+      w[e] = pack_codes(v[0][e] * vi, v[PER > 1 ? 1 : 0][e] * vi, v[PER > 2 ? 2 : 0][e] * vi, v[PER > 3 ? 3 : 0][e] * vi);
+    uint4* dst = (uint4*)vdst;
+    if (fresh != 0xFFFFFFFFu) {  // slots that are not this call's keep their codes, older ones at the new scale
+      uint32_t old[8];
+      *(uint4*)old = dst[0];
+      *(uint4*)(old + 4) = dst[1];
+      const int n = min(max(s0 - slot0, 0), 4);  // older slots
+      const uint32_t older = n ? 0xFFFFFFFFu >> (32 - 8 * n) : 0u;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      hi[e] = fmaxf(hi[e], __shfl_xor(hi[e], o, 64));
-      lo[e] = fminf(lo[e], __shfl_xor(lo[e], o, 64));
+      for (int e = 0; e < 8; ++e) {
+        if (vd < 0) old[e] = (rescale_codes(old[e], vd) & older) | (old[e] & ~older);
+        w[e] = (w[e] & fresh) | (old[e] & ~fresh);
+      }
     }
-  if (NW > 1 && lane < LPT)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      bred[0][wave][sub * 8 + e] = hi[e];
-      bred[1][wave][sub * 8 + e] = lo[e];
-    }
-  __syncthreads();
+    dst[0] = uint4{w[0], w[1], w[2], w[3]};
+    dst[1] = uint4{w[4], w[5], w[6], w[7]};
+  }
   if (tid < LPT) {
     int8_t* b = c.kb + ph * (2 * D) + sub * 8;
     __align__(8) int8_t bh[8], bl[8];
@@ -342,51 +390,19 @@ __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
           hi[e] = fmaxf(hi[e], bred[0][w][sub * 8 + e]);
           lo[e] = fminf(lo[e], bred[1][w][sub * 8 + e]);
         }
-      float nh = ceilf(hi[e] * 0.25f), nl = floorf(lo[e] * 0.25f);
+      const bool some = hi[e] >= lo[e];  // (a channel may hold NaN only)
+      const uint32_t w = pack_codes(some ? hi[e] * ki : 0.f, some ? lo[e] * ki : 0.f, 0.f, 0.f);
+      float nh = some ? ceilf(__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * 0.25f) : -128.f;
+      float nl = some ? floorf(__builtin_amdgcn_cvt_f32_fp8((int)w, 1) * 0.25f) : 127.f;
       if (s0 > 0) {
         nh = fmaxf(nh, ceilf(ldexpf((float)bh[e], kd)));
         nl = fminf(nl, floorf(ldexpf((float)bl[e], kd)));
       }
-      bh[e] = (int8_t)fmaxf(nh, -128.f);
-      bl[e] = (int8_t)fminf(nl, 127.f);
+      bh[e] = (int8_t)nh;
+      bl[e] = (int8_t)nl;
     }
     *(uint2*)b = *(uint2*)bh;
     *(uint2*)(b + D) = *(uint2*)bl;
-  }
-  // the values, four slots to a dword, 4 channels to a 16-byte store; slots that this call does not
-  // write keep their codes (older ones moved to the new scale)
-  const int q0 = vd < 0 ? 0 : s0 / 4, q1 = (s1 + 3) / 4;
-  for (int i = tid; i < (q1 - q0) * (D / 4); i += NT) {
-    const int quad = q0 + i / (D / 4), ch = i % (D / 4) * 4;
-    uint32_t r[4] = {0u, 0u, 0u, 0u};  // the quad's slots: 4 channels each
-    uint32_t fresh = 0u;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int slot = quad * 4 + e;
-      if (slot >= s0 && slot < s1) {
-        r[e] = *(const uint32_t*)&vt[slot - s0][ch];
-        fresh |= 0xFFu << (8 * e);
-      }
-    }
-    const uint32_t t0 = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), t1 = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);
-    const uint32_t t2 = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u), t3 = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
-    uint4 w{__builtin_amdgcn_perm(t2, t0, 0x05040100u), __builtin_amdgcn_perm(t2, t0, 0x07060302u),
-            __builtin_amdgcn_perm(t3, t1, 0x05040100u), __builtin_amdgcn_perm(t3, t1, 0x07060302u)};
-    uint4* dst = (uint4*)(vpage + quad * D + ch);
-    if (fresh != 0xFFFFFFFFu) {
-      const uint4 old = *dst;
-      uint32_t ow[4] = {old.x, old.y, old.z, old.w}, *nw = (uint32_t*)&w;
-      uint32_t older = 0u;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (quad * 4 + e < s0) older |= 0xFFu << (8 * e);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (vd < 0) ow[e] = (rescale_codes(ow[e], vd) & older) | (ow[e] & ~older);
-        nw[e] = (nw[e] & fresh) | (ow[e] & ~fresh);
-      }
-    }
-    *dst = w;
   }
   if (tid == 0) {
     c.ks[ph] = ldexpf(1.f, ke);
@@ -1273,13 +1289,14 @@ hipError_t qcache_append(const QCache& c, const QSegs& sg, const void* k, int64_
   // n tokens touch at most (n + 62) / 64 + 1 pages
   a.chunks = (max_new + 62) / PG + 1;
   const unsigned grid = (unsigned)a.chunks * c.H * sg.n_seg;
-  const int few = c.dh == 128 ? 4 : 8;  // tokens that one wave takes at once
+  // A wave holds 512 / D tokens, one to a group of lanes; a page of 64 takes a quad to a group of lanes.
+  const bool few = max_new <= 512 / c.dh;
   if (c.dh == 128) {
-    if (max_new <= few) k_qcache_append<128, 64, 1><<<grid, 64, 0, s>>>(a);
+    if (few) k_qcache_append<128, 64, 1><<<grid, 64, 0, s>>>(a);
     else k_qcache_append<128, 256, 4><<<grid, 256, 0, s>>>(a);
   } else {
-    if (max_new <= few) k_qcache_append<64, 64, 1><<<grid, 64, 0, s>>>(a);
-    else k_qcache_append<64, 256, 2><<<grid, 256, 0, s>>>(a);
+    if (few) k_qcache_append<64, 64, 1><<<grid, 64, 0, s>>>(a);
+    else k_qcache_append<64, 128, 4><<<grid, 128, 0, s>>>(a);
   }
   return hipGetLastError();
 }
