@@ -412,11 +412,10 @@ __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
 
 // ---------------------------------------------------------------------------
 // Attention.  A query's column c of a segment is head c % G of the KV head's group at token c / G.
-// A wave keeps QT tiles of 16 columns and walks 32-position steps, with the running maximum and sum
-// of each column in the lanes that hold it.  KEYS: the four waves share the columns and deal the
-// steps among them (few columns, the cache streams once); otherwise each wave has its own columns and
-// all walk the same steps (many columns; K/V come from the L1 for three waves of four).
-// PAIR (fp32 queries): queries and probabilities as fp16 pairs, about 22 bits.
+// A wave keeps its columns' running maximum and sum in the lanes that hold them and walks 32-position steps.  With few
+// columns (k_qcache_attend: QT tiles of 16) the four waves share them and deal the steps among themselves, so the cache
+// streams once; with many (k_qcache_attend_wide) each wave has its own and all walk the same steps, whose K/V come from
+// the L1 for three waves of four.  PAIR (fp32 queries): queries and probabilities as fp16 pairs, about 22 bits.
 
 struct AttendArgs {
   QCache c;
@@ -437,6 +436,61 @@ struct AttendArgs {
 
 template <int D> struct Step {  // a lane's K and V bytes of 32 positions
   uint4 k[2][D / 64], v[2][D / 64];
+};
+
+// The 32-position steps a wave takes: `from`, from + inc, ... below `end` of its row, or of the pages in `list`, that
+// begin below vmax and whose page lies in the pool.  Lane j holds page, position and scales of the j-th of 64 steps (a
+// bit of `todo` each), so that no step waits for the page table: one round trip for 64 steps.
+template <bool SEL> struct Walk {
+  const QCache& c;
+  const int32_t* list;
+  int row, h, lane, from, inc, end, vmax;
+  int lane_page, lane_pos;
+  float lane_ks, lane_vs;
+  uint64_t todo;
+  // the step that next() found
+  size_t ph;  // page * heads + head
+  int pos;
+  float ks, vs;
+  bool ok;
+
+  __device__ __forceinline__ void fill() {
+    const int st = from + lane * inc;
+    bool there = st < end;
+    if (there) {
+      int lp = st >> 1;
+      if (SEL) lp = list[lp];
+      lane_pos = lp * PG + 32 * (st & 1);
+      // (a position at or behind vmax: the last page's second half)
+      there = (unsigned)lp < (unsigned)c.ppr && lane_pos < vmax;
+      if (there) {
+        lane_page = c.pt[(size_t)row * c.ppr + lp];
+        there = (unsigned)lane_page < (unsigned)c.n_pages;
+        if (there) {
+          lane_ks = c.ks[(size_t)lane_page * c.H + h];
+          lane_vs = c.vs[(size_t)lane_page * c.H + h];
+        }
+      }
+    }
+    todo = __ballot(there);
+  }
+  __device__ __forceinline__ void next() {
+    while (todo == 0) {
+      from += 64 * inc;
+      if (from >= end) {
+        ok = false;
+        return;
+      }
+      fill();
+    }
+    const int j = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)todo) - 1);
+    todo &= todo - 1;
+    ph = (size_t)__builtin_amdgcn_readlane(lane_page, j) * c.H + h;
+    pos = __builtin_amdgcn_readlane(lane_pos, j);
+    ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_ks), j));
+    vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_vs), j));
+    ok = true;
+  }
 };
 
 // (Plain loads: non-temporal ones cost 4% over 64 ragged rows and 36% where tokens select the same pages.)
@@ -473,18 +527,21 @@ __device__ __forceinline__ int even_steps(const AttendArgs& a, int lane) {
   return __builtin_amdgcn_readfirstlane(max((total + a.splits - 1) / a.splits, QCACHE_LEAST_STEPS));
 }
 
-template <int D, int QT, bool PAIR, bool KEYS, bool SEL>
+// Probabilities are 2^(score - m + lift), m within `slack` of the running maximum: at most 2^14 in fp16, and rounded to
+// 11 bits down to 2^-28 of the largest.  Pairs keep their second halves above the subnormals by a larger lift.
+// (Eight prefixes of 1,500 to 2,048 tokens, 8 x 4 heads of 128, with no slack: 361 us, 333 with.)
+constexpr float slack_of(bool pair) { return pair ? 0.f : 10.f; }
+constexpr float lift_of(bool pair) { return pair ? 12.f : 4.f; }
+
+template <int D, int QT, bool PAIR, bool SEL>
 __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendArgs a) {
   constexpr int NS = D / 32, NJ = D / 16, CT = 16 * QT;
-  // Probabilities are 2^(score - m + LIFT), m within SLACK of the running maximum: at most 2^14 in fp16, and rounded to
-  // 11 bits down to 2^-28 of the largest.  Pairs keep their second halves above the subnormals by a larger LIFT.
-  // (Eight prefixes of 1,500 to 2,048 tokens, 8 x 4 heads of 128, with SLACK 0: 361 us.)
-  constexpr float SLACK = PAIR ? 0.f : 10.f, LIFT = PAIR ? 12.f : 4.f;
+  constexpr float SLACK = slack_of(PAIR), LIFT = lift_of(PAIR);
   const QCache& c = a.c;
   // block -> (split, column tile, head, segment[, token])
   int id = blockIdx.x;
   int split, tile, h, s, tokn = 0, per = a.per;
-  if (KEYS && !SEL && a.even) {
+  if (!SEL && a.even) {
     const int lane = threadIdx.x & 63;
     per = even_steps(a, lane);
     h = id % c.H; id /= c.H;
@@ -541,47 +598,18 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
   const int G = a.G, ncols = sg.n * G;
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int blockcol = tile * (KEYS ? CT : 4 * CT);
-  if (blockcol >= ncols) return;
-  const int col0 = KEYS ? blockcol : blockcol + wave * CT;
+  const int col0 = tile * CT;
+  if (col0 >= ncols) return;
 
-  // what the wave's first and its last column see (a wave without columns: nothing)
-  const bool idle = col0 >= ncols;
-  const int vmin = idle ? 0 : max(sg.p0 + col0 / G + 1, 0);
-  const int vmax = idle ? 0 : max(sg.p0 + (min(col0 + CT, ncols) - 1) / G + 1, 0);
+  // what the first and the last column see
+  const int vmin = max(sg.p0 + col0 / G + 1, 0);
+  const int vmax = max(sg.p0 + (min(col0 + CT, ncols) - 1) / G + 1, 0);
 
-  // 32-position steps of this split, and of this wave
-  const int32_t* list = SEL ? a.sel + ((size_t)sg.t0 * c.H + h) * a.n_sel : nullptr;
-  // (in KEYS mode every wave has the same columns; otherwise each stops at its own last position)
+  // 32-position steps of this split, dealt to the waves (with `per` from an estimate of the length the last split
+  // takes what a row has beyond it)
   const int steps = SEL ? 2 * a.n_sel : (vmax + 31) / 32;
-  // (with `per` from an estimate of the length the last split takes what a row has beyond it)
-  const int begin = split * per, inc = KEYS ? 4 : 1;
-  const int end = split == a.splits - 1 && !a.even ? steps : min(steps, begin + per);
-  // Lane j holds page, position and scales of the wave's j-th step from `from` on (a bit of `todo` each
-  // where there is a page), so that no step waits for the page table: one round trip for 64 steps.
-  int from = begin + (KEYS ? wave : 0), lane_page = 0, lane_pos = 0;
-  float lane_ks = 0.f, lane_vs = 0.f;
-  uint64_t todo = 0;
-  auto fill = [&] {
-    const int st = from + lane * inc;
-    bool ok = st < end;
-    if (ok) {
-      int lp = st >> 1;
-      if (SEL) lp = list[lp];
-      lane_pos = lp * PG + 32 * (st & 1);
-      // (a position at or behind vmax: the last page's second half)
-      ok = (unsigned)lp < (unsigned)c.ppr && lane_pos < vmax;
-      if (ok) {
-        lane_page = c.pt[(size_t)sg.row * c.ppr + lp];
-        ok = (unsigned)lane_page < (unsigned)c.n_pages;
-        if (ok) {
-          lane_ks = c.ks[(size_t)lane_page * c.H + h];
-          lane_vs = c.vs[(size_t)lane_page * c.H + h];
-        }
-      }
-    }
-    todo = __ballot(ok);
-  };
+  const int begin = split * per, end = split == a.splits - 1 && !a.even ? steps : min(steps, begin + per);
+  Walk<SEL> at{c, SEL ? a.sel + ((size_t)sg.t0 * c.H + h) * a.n_sel : nullptr, sg.row, h, lane, begin + wave, 4, end, vmax};
 
   f32x4 o[QT][NJ];
   float m[QT], l[QT];
@@ -597,33 +625,11 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
   bool first = true;
 
   Step<D> x;
-  int pos = 0, npos = 0;
-  float ks = 0.f, vs = 0.f, nks = 0.f, nvs = 0.f;
-  size_t nph = 0;
-  bool more, nmore;
-  // the next step: its page and head, position and scales
-  auto next = [&] {
-    while (todo == 0) {
-      from += 64 * inc;
-      if (from >= end) {
-        nmore = false;
-        return;
-      }
-      fill();
-    }
-    const int j = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)todo) - 1);
-    todo &= todo - 1;
-    nph = (size_t)__builtin_amdgcn_readlane(lane_page, j) * c.H + h;
-    npos = __builtin_amdgcn_readlane(lane_pos, j);
-    nks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_ks), j));
-    nvs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_vs), j));
-    nmore = true;
-  };
-  fill();
-  next();
-  if (nmore) {
-    load_k<D>(c, nph, (npos >> 5) & 1, lane, x.k);
-    load_v<D>(c, nph, (npos >> 5) & 1, lane, x.v);
+  at.fill();
+  at.next();
+  if (at.ok) {
+    load_k<D>(c, at.ph, (at.pos >> 5) & 1, lane, x.k);
+    load_v<D>(c, at.ph, (at.pos >> 5) & 1, lane, x.v);
   }
   // (the first positions are on their way)
   // queries: scaled by a power of two so that a column's largest element is in [2^10, 2^11)
@@ -678,15 +684,12 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
         if (PAIR) ql[t][k][e] = (f16)(y - (float)qh[t][k][e]);
       }
   }
-  more = nmore;
-  pos = npos;
-  ks = nks;
-  vs = nvs;
   // One step; EDGE: some of its positions are masked for a column, or lie behind the row's last one.
   auto step = [&](auto edge_tag) {
     constexpr bool EDGE = decltype(edge_tag)::value;
-    const int p0 = pos;
-    next();
+    const int p0 = at.pos;
+    const float ks = at.ks, vs = at.vs;
+    at.next();  // (the loads of the next step go out as its registers get free)
     // S^T = K Q^T
     f32x4 sc[QT][2];
 #pragma unroll
@@ -703,7 +706,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
           if (PAIR) sc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, ql[t][k], sc[t][n], 0, 0, 0);
         }
       }
-    if (nmore) load_k<D>(c, nph, (npos >> 5) & 1, lane, x.k);
+    if (at.ok) load_k<D>(c, at.ph, (at.pos >> 5) & 1, lane, x.k);
     // softmax of the 32 positions
     int ve = exponent_of(vs);
     if (first) vref = ve;
@@ -776,15 +779,11 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
         if (PAIR) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, pl8[t], o[t][j], 0, 0, 0);
       }
     }
-    if (nmore) load_v<D>(c, nph, (npos >> 5) & 1, lane, x.v);
-    more = nmore;
-    pos = npos;
-    ks = nks;
-    vs = nvs;
+    if (at.ok) load_v<D>(c, at.ph, (at.pos >> 5) & 1, lane, x.v);
   };
   // (positions increase, so the steps at the edge are the last ones; vmin <= len)
-  while (more && pos + 32 <= vmin) step(std::false_type{});
-  while (more) step(std::true_type{});
+  while (at.ok && at.pos + 32 <= vmin) step(std::false_type{});
+  while (at.ok) step(std::true_type{});
   const float unit = ldexpf(1.f, vref);
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -795,106 +794,295 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
   }
 
   constexpr int LD = D + 4;
-  if (KEYS) {  // the four waves' sums meet in LDS
-    // (32 columns: in two rounds, since four waves' sums take more than 64 KB)
-    constexpr int SLOTS = QT == 1 ? 4 : 2;
-    __shared__ __align__(16) float so[KEYS ? SLOTS * CT * LD : 4];
-    __shared__ float sm[4][CT], sl[4][CT];
-    const int live = min(ncols - blockcol, CT);
-    if (g == 0)
+  // the four waves' sums meet in LDS
+  // (32 columns: in two rounds, since four waves' sums take more than 64 KB)
+  constexpr int SLOTS = QT == 1 ? 4 : 2;
+  __shared__ __align__(16) float so[SLOTS * CT * LD];
+  __shared__ float sm[4][CT], sl[4][CT];
+  const int live = min(ncols - col0, CT);
+  if (g == 0)
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        sm[wave][16 * t + i] = m[t];
-        sl[wave][16 * t + i] = l[t];
-      }
+    for (int t = 0; t < QT; ++t) {
+      sm[wave][16 * t + i] = m[t];
+      sl[wave][16 * t + i] = l[t];
+    }
+  __syncthreads();
+  auto put = [&](int slot) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+      if (16 * t + i < live)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < NJ; j += 4)
+            *(f32x4*)&so[(slot * CT + 16 * t + i) * LD + (4 * g + r) * NJ + j] =
+                f32x4{o[t][j][r], o[t][j + 1][r], o[t][j + 2][r], o[t][j + 3][r]};
+  };
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) M = fmaxf(M, sm[w][16 * t + i]);
+    const float f = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - M);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) o[t][j] *= f;
+  }
+  if (SLOTS == 4) {
+    put(wave);
+  } else {
+    if (wave >= 2) put(wave - 2);
     __syncthreads();
-    auto put = [&](int slot) {
+    if (wave < 2)
 #pragma unroll
       for (int t = 0; t < QT; ++t)
         if (16 * t + i < live)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int j = 0; j < NJ; j += 4)
-              *(f32x4*)&so[(slot * CT + 16 * t + i) * LD + (4 * g + r) * NJ + j] =
-                  f32x4{o[t][j][r], o[t][j + 1][r], o[t][j + 2][r], o[t][j + 3][r]};
-    };
+            for (int j = 0; j < NJ; ++j) o[t][j][r] += so[(wave * CT + 16 * t + i) * LD + (4 * g + r) * NJ + j];
+    // each of the two waves writes where it alone has read
+    if (wave < 2) put(wave);
+  }
+  __syncthreads();
+  for (int k = tid; k < live * (D / 4); k += 256) {
+    const int cc = k / (D / 4), ch = k % (D / 4) * 4;
+    float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float M = -INFINITY;
+    for (int w = 0; w < 4; ++w) M = fmaxf(M, sm[w][cc]);
 #pragma unroll
-      for (int w = 0; w < 4; ++w) M = fmaxf(M, sm[w][16 * t + i]);
-      const float f = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - M);
+    for (int w = 0; w < 4; ++w) L += sm[w][cc] == -INFINITY ? 0.f : sl[w][cc] * __builtin_amdgcn_exp2f(sm[w][cc] - M);
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) o[t][j] *= f;
-    }
-    if (SLOTS == 4) {
-      put(wave);
+    for (int w = 0; w < SLOTS; ++w) y += *(const f32x4*)&so[(w * CT + cc) * LD + ch];
+    const int col = col0 + cc, tok = sg.t0 + col / G, head = h * G + col % G;
+    if (a.splits == 1) {
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+      store_row<4>(a.o, (int64_t)tok * a.ldo + (int64_t)head * D + ch, a.odt, a.alo, z, a.olo);
     } else {
-      if (wave >= 2) put(wave - 2);
-      __syncthreads();
-      if (wave < 2)
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-          if (16 * t + i < live)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-              for (int j = 0; j < NJ; ++j) o[t][j][r] += so[(wave * CT + 16 * t + i) * LD + (4 * g + r) * NJ + j];
-      // each of the two waves writes where it alone has read
-      if (wave < 2) put(wave);
-    }
-    __syncthreads();
-    for (int k = tid; k < live * (D / 4); k += 256) {
-      const int cc = k / (D / 4), ch = k % (D / 4) * 4;
-      float M = -INFINITY, L = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) M = fmaxf(M, sm[w][cc]);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) L += sm[w][cc] == -INFINITY ? 0.f : sl[w][cc] * __builtin_amdgcn_exp2f(sm[w][cc] - M);
-      f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < SLOTS; ++w) y += *(const f32x4*)&so[(w * CT + cc) * LD + ch];
-      const int col = blockcol + cc, tok = sg.t0 + col / G, head = h * G + col % G;
-      if (a.splits == 1) {
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
-        store_row<4>(a.o, (int64_t)tok * a.ldo + (int64_t)head * D + ch, a.odt, a.alo, z, a.olo);
-      } else {
-        float* p = a.part + (((size_t)tok * (c.H * G) + head) * a.splits + split) * LD;
-        *(f32x4*)(p + ch) = y;
-        if (ch == 0) {
-          p[D] = M;
-          p[D + 1] = L;
-        }
+      float* p = a.part + (((size_t)tok * (c.H * G) + head) * a.splits + split) * LD;
+      *(f32x4*)(p + ch) = y;
+      if (ch == 0) {
+        p[D] = M;
+        p[D + 1] = L;
       }
     }
+  }
+}
+
+// Many columns: each of the workgroup's four waves has 32 of its own, and all walk the same steps.  One 32x32x16
+// product takes 32 positions (or channels) by 32 columns:
+//   lane l = 32 f + i:  A row i, B column i, k slots 8 f .. 8 f + 7,  C column i, rows 8 (r / 4) + 4 f + r % 4
+//   S^T: A row i = position i, k slots of step s = channels f D/2 + 8 s ..
+//   O^T tile j: A row i = channel i D/32 + j; of half u of the positions, k slots = positions 16 u + 4 f .. + 3 and
+//     16 u + 8 + 4 f .. + 3: two dwords of the value page, and scores 8 u .. 8 u + 7 of the lane
+// so a lane has one column, and half the instructions around the products of the 16-column kernel.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int D, bool PAIR>
+__global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
+  constexpr int NS = D / 16, NJ = D / 32, LD = D + 4;
+  constexpr float SLACK = slack_of(PAIR), LIFT = lift_of(PAIR);
+  const QCache& c = a.c;
+  int id = blockIdx.x, pair;
+  const int x = id & 7;
+  if (a.by_xcd) id >>= 3;
+  const int split = id % a.splits;
+  id /= a.splits;
+  if (a.by_xcd) {
+    // Blocks go to the 8 XCDs in turn; those of one (segment, head) pair follow each other on one XCD and
+    // read the same pages through its L2.  The tiles with the most positions go first.
+    pair = id / a.tiles * 8 + x;
+    id %= a.tiles;
   } else {
+    pair = id % (a.sg.n_seg * c.H);
+    id /= a.sg.n_seg * c.H;
+  }
+  if (pair >= a.sg.n_seg * c.H) return;
+  const int h = pair % c.H, tile = a.tiles - 1 - id;
+  const Seg sg = seg_of(a.sg, pair / c.H, c.rows, c.ppr * PG);
+  const int G = a.G, ncols = sg.n * G;
+  const int lane = threadIdx.x & 63, i = lane & 31, f = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col0 = tile * 128 + wave * 32;
+  if (col0 >= ncols) return;
+  const int vmin = max(sg.p0 + col0 / G + 1, 0);
+  const int vmax = max(sg.p0 + (min(col0 + 32, ncols) - 1) / G + 1, 0);
+  const int steps = (vmax + 31) / 32, begin = split * a.per;
+  Walk<false> at{c, nullptr, sg.row, h, lane, begin, 1, split == a.splits - 1 ? steps : min(steps, begin + a.per), vmax};
+
+  uint4 kb[D / 32];
+  uint32_t vb[4][NJ];  // of quads f, 2 + f, 4 + f and 6 + f
+  auto load_keys = [&] {
+    const uint8_t* p = c.k + at.ph * (PG * D) + ((at.pos >> 5) & 1) * (32 * D) + i * D + f * (D / 2);
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      if (tokc[t] < 0) continue;
-      if (a.splits == 1) {
-        const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];
+    for (int e = 0; e < D / 32; ++e) kb[e] = *(const uint4*)(p + 16 * e);
+  };
+  auto load_values = [&] {
+    const uint8_t* p = c.v + at.ph * (PG * D) + ((at.pos >> 5) & 1) * (32 * D) + f * (4 * D) + i * (4 * NJ);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float z[NJ];
+    for (int e = 0; e < 4; ++e) {
+      if (NJ == 4) *(uint4*)vb[e] = *(const uint4*)(p + e * 8 * D);
+      else *(uint2*)vb[e] = *(const uint2*)(p + e * 8 * D);
+    }
+  };
+  at.fill();
+  at.next();
+  if (at.ok) {
+    load_keys();
+    load_values();
+  }
+
+  // the query, scaled by a power of two so that its largest element is in [2^10, 2^11)
+  const int col = col0 + i;
+  const bool live = col < ncols;
+  const int tok = sg.t0 + (live ? col / G : 0), head = h * G + (live ? col % G : 0);
+  const int vis = live ? sg.p0 + col / G + 1 : 0;
+  half8 qh[NS], ql[PAIR ? NS : 1];
+  float cq;
+  {
+    float y[NS][8], top = 0.f;
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) z[j] = o[t][j][r] * inv;
-          store_row<NJ>(a.o, (int64_t)tokc[t] * a.ldo + (int64_t)headc[t] * D + (4 * g + r) * NJ, a.odt, a.alo, z, a.olo);
+    for (int k = 0; k < NS; ++k) {
+      if (live) load8(a.q, (int64_t)tok * a.ldq + (int64_t)head * D + f * (D / 2) + k * 8, a.dt, a.alq, y[k]);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[k][e] = 0.f;
+    }
+    if (a.rope) {
+      const float2* tab = a.rope + (size_t)min(max(vis - 1, 0), c.ppr * PG - 1) * (D / 2);
+#pragma unroll
+      for (int k = 0; k < NS; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float other = __shfl_xor(y[k][e], 32, 64);
+          const float2 cs = tab[k * 8 + e];
+          float lo, hi;
+          rope_pair(f ? other : y[k][e], f ? y[k][e] : other, cs.x, cs.y, lo, hi);
+          y[k][e] = f ? hi : lo;
         }
-      } else {
-        float* p = a.part + (((size_t)tokc[t] * (c.H * G) + headc[t]) * a.splits + split) * LD;
+    }
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+    for (int k = 0; k < NS; ++k)
 #pragma unroll
-          for (int j = 0; j < NJ; j += 4)
-            *(f32x4*)(p + (4 * g + r) * NJ + j) = f32x4{o[t][j][r], o[t][j + 1][r], o[t][j + 2][r], o[t][j + 3][r]};
-        if (g == 0) {
-          p[D] = m[t];
-          p[D + 1] = l[t];
-        }
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(y[k][e]));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    int ex;
+    frexpf(top, &ex);
+    if (!(top > 0.f)) ex = 0;
+    cq = ldexpf(a.scale * QC_LOG2E, ex - 11);
+#pragma unroll
+    for (int k = 0; k < NS; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float z = ldexpf(y[k][e], 11 - ex);
+        qh[k][e] = (f16)z;
+        if (PAIR) ql[k][e] = (f16)(z - (float)qh[k][e]);
+      }
+  }
+
+  f32x16 o[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[j][r] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  int vref = 0;  // o is in units of 2^vref
+  bool first = true;
+  auto step = [&](auto edge_tag) {
+    constexpr bool EDGE = decltype(edge_tag)::value;
+    const int p0 = at.pos;
+    const float cs = fmaxf(cq * at.ks, 1e-37f);  // (not 0: -inf stays -inf)
+    const int ve = exponent_of(at.vs);
+    at.next();
+    f32x16 sc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NS; ++k) {
+      const uint4 w = kb[k / 2];
+      const half8 A = k & 1 ? codes_f16(w.z, w.w, 1.f) : codes_f16(w.x, w.y, 1.f);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, qh[k], sc, 0, 0, 0);
+      if (PAIR) sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, ql[k], sc, 0, 0, 0);
+    }
+    if (at.ok) load_keys();
+    if (first) vref = ve;
+    first = false;
+    float fall = 1.f;  // o to another unit where the page's scale is far from it
+    if (ve - vref > 4 || ve - vref < -6) {
+      fall = ldexpf(1.f, vref - ve);
+      vref = ve;
+    }
+    const float vr = ldexpf(1.f, ve - vref);
+    float top = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      if (EDGE && p0 + 8 * (r / 4) + 4 * f + r % 4 >= vis) sc[r] = -INFINITY;
+      top = fmaxf(top, sc[r]);
+    }
+    top *= cs;
+    if (__any(top > m + SLACK) || fall != 1.f) {
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float nm = top > m + SLACK ? top : m;
+      const float al = nm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - nm);
+      l *= al;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) o[j] *= al * fall;
+      m = nm;
+    }
+    const float base = m == -INFINITY ? 0.f : m - LIFT;
+    half8 ph8[2], pl8[PAIR ? 2 : 1];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(sc[r], cs, -base));
+      l += p;
+      ph8[r / 8][r % 8] = (f16)p;
+      if (PAIR) pl8[r / 8][r % 8] = (f16)(p - (float)ph8[r / 8][r % 8]);
+    }
+    if (EDGE) {  // codes behind the row's last position may be anything
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int left = min(max(sg.len - (p0 + 8 * e + 4 * f), 0), 4);
+        const uint32_t keep = left == 4 ? 0xFFFFFFFFu : (1u << (8 * left)) - 1u;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) vb[e][j] &= keep;
       }
     }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const half8 A = codes_f16(vb[2 * u][j], vb[2 * u + 1][j], vr);
+        o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, ph8[u], o[j], 0, 0, 0);
+        if (PAIR) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, pl8[u], o[j], 0, 0, 0);
+      }
+    if (at.ok) load_values();
+  };
+  while (at.ok && at.pos + 32 <= vmin) step(std::false_type{});
+  while (at.ok) step(std::true_type{});
+  l += __shfl_xor(l, 32, 64);
+  if (!live) return;
+  const float out = a.splits > 1 ? ldexpf(1.f, vref) : l == 0.f ? 0.f : ldexpf(1.f, vref) / l;
+  float* part = a.part + (((size_t)tok * (c.H * G) + head) * a.splits + split) * LD;
+#pragma unroll
+  for (int r = 0; r < 16; r += 2) {  // two rows' channels follow each other
+    const int ch = (8 * (r / 4) + 4 * f + r % 4) * NJ;
+    float z[2 * NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      z[j] = o[j][r] * out;
+      z[NJ + j] = o[j][r + 1] * out;
+    }
+    if (a.splits == 1) {
+      store_row<2 * NJ>(a.o, (int64_t)tok * a.ldo + (int64_t)head * D + ch, a.odt, a.alo, z, a.olo);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 2 * NJ; e += 4) *(f32x4*)(part + ch + e) = f32x4{z[e], z[e + 1], z[e + 2], z[e + 3]};
+    }
+  }
+  if (a.splits > 1 && f == 0) {
+    part[D] = m;
+    part[D + 1] = l;
   }
 }
 
@@ -1311,10 +1499,10 @@ static hipError_t attend_launch(const QAttendPlan& p, AttendArgs& a, hipStream_t
   const unsigned pairs = (unsigned)a.sg.n_seg * a.c.H;
   const unsigned grid = p.even ? a.c.H * p.tiles * (p.splits + a.sg.n_seg)
                                : (a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * p.tiles * p.splits * (a.sel ? a.sg.max_new : 1);
-  if (a.sel) k_qcache_attend<D, 1, PAIR, true, true><<<grid, 256, 0, s>>>(a);
-  else if (!p.keys) k_qcache_attend<D, 2, PAIR, false, false><<<grid, 256, 0, s>>>(a);
-  else if (p.qt == 1) k_qcache_attend<D, 1, PAIR, true, false><<<grid, 256, 0, s>>>(a);
-  else k_qcache_attend<D, 2, PAIR, true, false><<<grid, 256, 0, s>>>(a);
+  if (a.sel) k_qcache_attend<D, 1, PAIR, true><<<grid, 256, 0, s>>>(a);
+  else if (!p.keys) k_qcache_attend_wide<D, PAIR><<<grid, 256, 0, s>>>(a);
+  else if (p.qt == 1) k_qcache_attend<D, 1, PAIR, false><<<grid, 256, 0, s>>>(a);
+  else k_qcache_attend<D, 2, PAIR, false><<<grid, 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const size_t items = (size_t)a.sg.n_seg * a.sg.max_new * a.c.H * a.G;
