@@ -190,10 +190,12 @@ ams_status ams_index_hash_noalloc(const void* data, size_t n_bytes, int32_t seg_
  * block of 64 positions (a page) and head: half the bytes of an fp16 cache, so
  * twice the contexts fit the GPU (paper section 3.2.2, Layered Storage of
  * Action Context) and a decode step, which streams the cache, reads half.
- * All arrays are on the current device, 16-byte aligned, owned by the caller:
+ * All arrays are on the current device and owned by the caller; k, v and k_bounds
+ * 16-byte aligned:
  *   k        [n_pages][n_kv_heads][64][head_dim]     e4m3 codes
  *   v        [n_pages][n_kv_heads][16][head_dim][4]  e4m3 codes, position t of a
- *            page at [t / 4][:][t % 4]
+ *            page at [t / 4][:][t % 4]; no NaN among the positions in use
+ *            (an append writes none)
  *   k_scale, v_scale  fp32 [n_pages][n_kv_heads], powers of two: a code stands for
  *            its value times its page's scale
  *   k_bounds int8 [n_pages][n_kv_heads][2][head_dim]: per channel the largest
@@ -318,10 +320,12 @@ void ams_ctx_destroy(ams_ctx* c); /* NULL is a no-op */
  * that are as much smaller.  Builds, appends, steps and flow append to it and
  * attend over it (a row's own new tokens too, so a step gives what a rebuilt
  * context gives but for the codes that a growing scale rounded again); the action
- * decode runs as per-layer kernels.  Keys and values carry 4 significant bits:
- * logits differ from an fp16 context's by that much.  Scratch positions that a step
- * drops can leave a page's scale and bounds larger than its committed positions
- * need.  See ams_qcache_append and ams_ctx_select_pages. */
+ * decode runs as per-layer kernels, which suits many rows and long contexts (one row
+ * of a few hundred positions is faster in an fp16 context's persistent decode).
+ * Keys and values carry 4 significant bits: logits differ from an fp16 context's
+ * by that much.  Scratch positions that a step or a flow drops can leave a page's
+ * scale and bounds larger than its committed positions need.  See ams_qcache_append
+ * and ams_ctx_select_pages. */
 #define AMS_CTX_QCACHE 2
 
 /* Bytes of workspace of a paged context: as ams_ctx_workspace_bytes with

@@ -551,14 +551,13 @@ bool qcache_tensor(const void* p, int64_t ld, int32_t n_tok, int64_t width, int3
 }
 
 bool qcache_arrays(const ams_qcache* c, const int32_t* tok_off, const int32_t* kv_len, DevRanges& in, std::string& e) {
-  const void* p[] = {c->k, c->v, c->k_scale, c->v_scale, c->k_bounds};
-  for (const void* x : p)
-    if ((uintptr_t)x & 15) {
-      e = "the cache's arrays must be 16-byte aligned";
-      return false;
-    }
-  if (((uintptr_t)c->page_table | (uintptr_t)tok_off | (uintptr_t)kv_len) & 3) {
-    e = "page_table, tok_off and kv_len must be 4-byte aligned";
+  if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->k_bounds) & 15) {
+    e = "the cache's k, v and k_bounds must be 16-byte aligned";
+    return false;
+  }
+  if (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale | (uintptr_t)c->page_table | (uintptr_t)tok_off |
+       (uintptr_t)kv_len) & 3) {
+    e = "scales, page_table, tok_off and kv_len must be 4-byte aligned";
     return false;
   }
   const size_t ph = (size_t)c->n_pages * c->n_kv_heads, d = c->head_dim;
@@ -629,9 +628,9 @@ ams_status ams_qcache_attend(const ams_qcache* cache, const int32_t* tok_off, co
   if (n_tok == 0) return AMS_OK;
   const ams::QAttendPlan p = qcache_plan(cache, n_heads, n_tok, max_new, max_len, n_select);
   max_new = std::min(max_new, n_tok);
-  const int64_t heads = (int64_t)cache->rows * n_heads * max_new;
-  if (heads > 4 * QCACHE_MAX_BLOCKS || p.blocks > QCACHE_MAX_BLOCKS)
-    return fail(AMS_EINVAL, "too many queries for one call: rows * max_new * n_heads is above 2^24");
+  if (p.blocks > QCACHE_MAX_BLOCKS ||
+      (p.splits > 1 && (int64_t)cache->rows * n_heads * max_new > 4 * QCACHE_MAX_BLOCKS))
+    return fail(AMS_EINVAL, "too many queries for one call: rows * n_kv_heads * max_new needs more than 2^22 workgroups");
   const size_t list = (size_t)n_tok * cache->n_kv_heads * n_select * 4, part = align16(p.part_floats * 4);
   const size_t need = part + (selected ? 0 : list);
   if (need && !ws) return fail(AMS_EINVAL, "ws is NULL");

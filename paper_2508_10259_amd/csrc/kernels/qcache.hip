@@ -532,6 +532,14 @@ __device__ __forceinline__ int even_steps(const AttendArgs& a, int lane) {
 // (Eight prefixes of 1,500 to 2,048 tokens, 8 x 4 heads of 128, with no slack: 361 us, 333 with.)
 constexpr float slack_of(bool pair) { return pair ? 0.f : 10.f; }
 constexpr float lift_of(bool pair) { return pair ? 12.f : 4.f; }
+// fp16 probabilities are summed as they enter the product, rounded, so that their weights add up to one: a query that
+// one position dominates gets that position's value exactly.  1 * p + l with an opaque 1 is one instruction (a fused
+// multiply-add of an fp16 operand) where a conversion and an addition are two.
+__device__ __forceinline__ float opaque_one() {
+  float one = 1.f;
+  asm("" : "+v"(one));
+  return one;
+}
 
 template <int D, int QT, bool PAIR, bool SEL>
 __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendArgs a) {
@@ -684,6 +692,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
         if (PAIR) ql[t][k][e] = (f16)(y - (float)qh[t][k][e]);
       }
   }
+  const float one = opaque_one();
   // One step; EDGE: some of its positions are masked for a column, or lie behind the row's last one.
   auto step = [&](auto edge_tag) {
     constexpr bool EDGE = decltype(edge_tag)::value;
@@ -747,9 +756,13 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float p = __builtin_amdgcn_exp2f(fmaf(sc[t][n][r], cs, -base));
-          l[t] += p;
           ph8[t][4 * n + r] = (f16)p;
-          if (PAIR) pl8[t][4 * n + r] = (f16)(p - (float)ph8[t][4 * n + r]);
+          if (PAIR) {
+            pl8[t][4 * n + r] = (f16)(p - (float)ph8[t][4 * n + r]);
+            l[t] += p;
+          } else {
+            l[t] = fmaf((float)ph8[t][4 * n + r], one, l[t]);
+          }
         }
     }
     // O^T += V^T P^T; codes behind the row's last position may be anything
@@ -989,6 +1002,7 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
   float m = -INFINITY, l = 0.f;
   int vref = 0;  // o is in units of 2^vref
   bool first = true;
+  const float one = opaque_one();
   auto step = [&](auto edge_tag) {
     constexpr bool EDGE = decltype(edge_tag)::value;
     const int p0 = at.pos;
@@ -1035,9 +1049,13 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float p = __builtin_amdgcn_exp2f(fmaf(sc[r], cs, -base));
-      l += p;
       ph8[r / 8][r % 8] = (f16)p;
-      if (PAIR) pl8[r / 8][r % 8] = (f16)(p - (float)ph8[r / 8][r % 8]);
+      if (PAIR) {
+        pl8[r / 8][r % 8] = (f16)(p - (float)ph8[r / 8][r % 8]);
+        l += p;
+      } else {
+        l = fmaf((float)ph8[r / 8][r % 8], one, l);
+      }
     }
     if (EDGE) {  // codes behind the row's last position may be anything
 #pragma unroll

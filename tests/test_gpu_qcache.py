@@ -349,6 +349,42 @@ def test_selection_ties_and_missing_pages():
     b.attend((3,), 2, "f32", n_select=9, std=0.0)
 
 
+def test_selection_over_the_widest_table():
+    """16,384 pages a row, of which a few dozen lie in the pool: the keys take more LDS than a kernel has by
+    default, and most pages cannot be chosen."""
+    table = np.full((2, 16384), -1, np.int32)
+    rng = np.random.default_rng(23)
+    at = [np.sort(rng.choice(16383, 39, replace=False)) for _ in range(2)]
+    for r in range(2):
+        table[r, at[r]], table[r, 16383] = np.arange(40 * r, 40 * r + 39), 40 * r + 39
+    b = Both(2, 40, 1, 64, seed=24, table=np.arange(80, dtype=np.int32).reshape(2, 40), spare=0)
+    b.append((40 * 64, 40 * 64), "f16")
+    import torch
+    from paper_2508_10259_amd.qcache import QuantCache
+    b.ref.table, b.lens = table, [16384 * 64, 16384 * 64 - 70]
+    d = b.dev
+    b.dev = QuantCache(d.k, d.v, d.k_scale, d.v_scale, d.k_bounds, torch.from_numpy(table).cuda())
+    for n in (1, 7, 39, 64):
+        b.attend((1, 1), 2, "f16", n_select=n)
+    b.attend((2, 1), 1, "f32", n_select=5)
+
+
+def test_arrays_cut_out_of_stacks_of_layers():
+    """One layer of stacked pools, whose scales start at an odd multiple of 4 bytes."""
+    import torch
+    from paper_2508_10259_amd.qcache import QuantCache
+    b = Both(2, 2, 3, 64, seed=25, spare=1)
+    d, L = b.dev, 3
+    stack = lambda t: torch.stack([t.view(torch.uint8) if t.dtype == d.k.dtype else t] * L)  # noqa: E731
+    parts = [stack(t)[1] for t in (d.k, d.v, d.k_scale, d.v_scale, d.k_bounds)]
+    b.dev = QuantCache(parts[0].view(d.k.dtype), parts[1].view(d.k.dtype), *parts[2:], d.page_table)
+    assert b.dev.k_scale.data_ptr() % 16
+    b.append((70, 5), "bf16")
+    b.check()
+    b.attend((1, 3), 2, "bf16")
+    b.attend((1, 3), 2, "bf16", n_select=1)
+
+
 # --- together -------------------------------------------------------------------------------------
 
 
