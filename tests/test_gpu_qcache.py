@@ -349,6 +349,25 @@ def test_selection_ties_and_missing_pages():
     b.attend((3,), 2, "f32", n_select=9, std=0.0)
 
 
+def test_selection_ties_among_hundreds_of_pages():
+    import torch
+    rng = np.random.default_rng(26)
+    table = np.arange(700, dtype=np.int32)[None].copy()
+    table[0, rng.choice(699, 60, replace=False)] = -1
+    b = Both(1, 700, 1, 64, seed=27, table=table, spare=0)
+    b.append((700 * 64 - 9,), "f16")
+    # five promises, shared by many pages each
+    kind = rng.integers(0, 5, b.ref.bounds.shape[0])
+    b.ref.bounds[:] = b.ref.bounds[kind]
+    b.dev.k_bounds.copy_(torch.from_numpy(b.ref.bounds.astype(np.int8)))
+    b.ref.ke[:] = -7
+    b.dev.k_scale.fill_(2.0 ** -7)
+    for n in (1, 2, 100, 200, 639, 640, 641):
+        b.attend((1,), 2, "f16", n_select=n)
+    b.attend((2,), 2, "f16", n_select=130)
+    b.attend((1,), 2, "f32", n_select=9, std=0.0)
+
+
 def test_selection_over_the_widest_table():
     """16,384 pages a row, of which a few dozen lie in the pool: the keys take more LDS than a kernel has by
     default, and most pages cannot be chosen."""
