@@ -2,16 +2,16 @@
 //
 // Layout.  A page holds 64 positions of every head of one layer.  Keys are rows [64][D] of
 // e4m3; values are stored four positions to a dword, [16][D][4].  With keys as the A operand
-// of S^T = K Q^T and values as the A operand of O^T = V^T P^T every lane of a wave reads its
-// fragments as 16-byte loads of contiguous memory, and the probabilities leave the first
-// product in the registers the second one reads: no transposition and no LDS on the way.
+// of S^T = K Q^T and values as the A operand of O^T = V^T P^T a lane's fragments are whole
+// 16-byte words of either page, and the probabilities leave the first product in the registers
+// the second one reads: nothing is transposed.
 //   16x16x32 product, lane l = 16 g + i:  A row i, B column i, k slots 8 g .. 8 g + 7,
 //   C column i, rows 4 g .. 4 g + 3.
 //   S^T tile t of a 32-position step: A row i = position 16 t + i, k slots of step s = channels
 //     g D/4 + 8 s .. + 7 (both operands agree on that order); the lane gets the scores of query i
 //     at positions 16 t + 4 g + r.
-//   O^T tile j: A row i = channel i D/16 + j, k slots of group g = positions 4 g .. 4 g + 3 of
-//     tile 0, then of tile 1: one dword of the value page each, and the lane's own scores.
+//   O^T tile j: A row i = channel 64 (j / 4) + 4 i + j % 4, k slots of group g = positions 4 g ..
+//     4 g + 3 of tile 0, then of tile 1: one dword of the value page each, and the lane's own scores.
 // A scale is a power of two: e4m3 keeps its three mantissa bits at any exponent, so a finer scale
 // would not round better, and moving a page to a larger scale is exact but for subnormals.
 #include <algorithm>
@@ -167,8 +167,11 @@ __device__ __forceinline__ uint32_t rescale_codes(uint32_t w, int de) {
 // ---------------------------------------------------------------------------
 // Append.  One workgroup per (page, head): it alone writes that page's codes, scales and bounds.
 // D/8 lanes take a quad of slots, 8 channels each: a lane's four values of a channel are one dword of the value page,
-// its four keys 8 bytes of their rows.  With few tokens they take one slot, and a value is a byte of that dword.  The tokens stay in registers from the maximum, which sets the scale, to the
-// rounding.
+// its four keys 8 bytes of their rows.  With few tokens they take one slot, and a value is a byte of that dword.  The
+// tokens stay in registers from the maximum, which sets the scale, to the rounding.
+// Measured: 64 prefixes of 200 to 400 tokens, 32 heads of 128, bf16 with rotation: 136 us for 0.48 GB, 3.5 TB/s (a
+// large copy: 4.85); the chain load, maximum, round, store bounds it, four waves a SIMD deep.  One token for each of 64
+// rows: 7 us, a launch and four dependent round trips.
 
 // The least e >= -32 with a <= 448 2^e (448 = 0.875 * 2^9).
 __device__ __forceinline__ int scale_exponent(float a) {
@@ -416,6 +419,9 @@ __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
 // columns (k_qcache_attend: QT tiles of 16) the four waves share them and deal the steps among themselves, so the cache
 // streams once; with many (k_qcache_attend_wide) each wave has its own and all walk the same steps, whose K/V come from
 // the L1 for three waves of four.  PAIR (fp32 queries): queries and probabilities as fp16 pairs, about 22 bits.
+// Measured: few columns are bound by memory (4 rows of 70,000 to 131,000 positions, 8 x 4 heads of 128: 152 us for 0.82
+// GB, 5.4 TB/s; 64 rows of 200 to 768 positions, 32 heads: 51 us for 0.25 GB), many by the vector unit and the products
+// of the same waves taking turns (eight prefixes of 1,500 to 2,048 tokens, 8 x 4 heads: 291 us, 0.72 PFLOP/s).
 
 struct AttendArgs {
   QCache c;
@@ -435,7 +441,8 @@ struct AttendArgs {
 };
 
 template <int D> struct Step {  // a lane's K and V bytes of 32 positions
-  uint4 k[2][D / 64], v[2][D / 64];
+  i32x4 k[D / 32];
+  uint4 v[2][D / 64];
 };
 
 // The 32-position steps a wave takes: `from`, from + inc, ... below `end` of its row, or of the pages in `list`, that
@@ -448,7 +455,8 @@ template <bool SEL> struct Walk {
   int lane_page, lane_pos;
   float lane_ks, lane_vs;
   uint64_t todo;
-  // the step that next() found
+  // the step that find() found, lane j's
+  int j;
   size_t ph;  // page * heads + head
   int pos;
   float ks, vs;
@@ -474,7 +482,11 @@ template <bool SEL> struct Walk {
     }
     todo = __ballot(there);
   }
-  __device__ __forceinline__ void next() {
+  // Waits for fill's scales.  Left to their first use, which may or may not follow a fill, the wait would be for every
+  // load in flight, the next step's K and V among them, in every step.  (This and `step` without conditions around its
+  // loads: eight prefixes of 1,500 to 2,048 tokens, 8 x 4 heads of 128, 320 -> 291 us.)
+  __device__ __forceinline__ void settle() { asm volatile("" : "+v"(lane_ks), "+v"(lane_vs)); }
+  __device__ __forceinline__ void find() {
     while (todo == 0) {
       from += 64 * inc;
       if (from >= end) {
@@ -482,33 +494,57 @@ template <bool SEL> struct Walk {
         return;
       }
       fill();
+      settle();
     }
-    const int j = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)todo) - 1);
+    j = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)todo) - 1);
     todo &= todo - 1;
     ph = (size_t)__builtin_amdgcn_readlane(lane_page, j) * c.H + h;
     pos = __builtin_amdgcn_readlane(lane_pos, j);
+    ok = true;
+  }
+  __device__ __forceinline__ void scales() {
     ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_ks), j));
     vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lane_vs), j));
-    ok = true;
+  }
+  __device__ __forceinline__ void next() {
+    find();
+    if (ok) scales();
   }
 };
 
 // (Plain loads: non-temporal ones cost 4% over 64 ragged rows and 36% where tokens select the same pages.)
 template <int D>
-__device__ __forceinline__ void load_k(const QCache& c, size_t ph, int half, int lane, uint4 (&k)[2][D / 64]) {
-  const uint8_t* p = c.k + ph * (PG * D) + half * (32 * D) + (lane & 15) * D + (lane >> 4) * (D / 4);
+__device__ __forceinline__ void load_k(const QCache& c, size_t ph, int half, int lane, i32x4 (&k)[D / 32]) {
+  const uint8_t* p = c.k + (ph * (PG * D) + half * (32 * D));
+  const uint32_t at = lane * 16u;
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int e = 0; e < D / 32; ++e) k[e] = *(const i32x4*)(p + at + e * 1024);
+}
+// A product wants a key to a lane, and 16-byte loads whose neighbouring lanes are in different rows pass the L1 at a
+// quarter of its rate (measured: 15.7 bytes a cycle and CU, 59 with neighbours side by side).  So a wave loads its 32
+// keys as they lie in memory, and turns them in LDS of its own: the 16-byte pieces of a row are permuted so that eight
+// lanes meet all banks, in the writes (one row, or two of 64) and in the reads (eight rows' pieces).  4 x 48 new tokens
+// over 32 selected pages each, 8 x 4 heads of 128, where pages come from the L2: 84 us without, 68 with.
+template <int D>
+__device__ __forceinline__ int k_slot(int row, int piece) {
+  return row * D + (piece ^ (D == 128 ? row & 7 : (row >> 1) & 3)) * 16;
+}
+template <int D>
+__device__ __forceinline__ void turn_k(const i32x4 (&k)[D / 32], char* lds, int lane) {
+  constexpr int PR = D / 16;  // pieces of a row
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (lanes read what others wrote)
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) k[t][e] = *(const uint4*)(p + t * 16 * D + e * 16);
+  for (int e = 0; e < D / 32; ++e) *(i32x4*)(lds + k_slot<D>(e * (64 / PR) + lane / PR, lane % PR)) = k[e];
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 template <int D>
 __device__ __forceinline__ void load_v(const QCache& c, size_t ph, int half, int lane, uint4 (&v)[2][D / 64]) {
-  const uint8_t* p = c.v + ph * (PG * D) + half * (32 * D) + (lane >> 4) * (4 * D) + (lane & 15) * (D / 4);
+  const uint8_t* p = c.v + (ph * (PG * D) + half * (32 * D));
+  const uint32_t at = (lane >> 4) * (4u * D) + (lane & 15) * 16u;
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) v[t][e] = *(const uint4*)(p + t * 16 * D + e * 16);
+    for (int e = 0; e < D / 64; ++e) v[t][e] = *(const uint4*)(p + at + t * 16 * D + e * 256);
 }
 
 // The 32-position steps that segment s's last token sees.
@@ -529,20 +565,20 @@ __device__ __forceinline__ int even_steps(const AttendArgs& a, int lane) {
 
 // Probabilities are 2^(score - m + lift), m within `slack` of the running maximum: at most 2^14 in fp16, and rounded to
 // 11 bits down to 2^-28 of the largest.  Pairs keep their second halves above the subnormals by a larger lift.
-// (Eight prefixes of 1,500 to 2,048 tokens, 8 x 4 heads of 128, with no slack: 361 us, 333 with.)
+// (Eight prefixes of 1,500 to 2,048 tokens, 8 x 4 heads of 128: 361 us with no slack when 333 with it.)
 constexpr float slack_of(bool pair) { return pair ? 0.f : 10.f; }
 constexpr float lift_of(bool pair) { return pair ? 12.f : 4.f; }
 // fp16 probabilities are summed as they enter the product, rounded, so that their weights add up to one: a query that
-// one position dominates gets that position's value exactly.  1 * p + l with an opaque 1 is one instruction (a fused
-// multiply-add of an fp16 operand) where a conversion and an addition are two.
-__device__ __forceinline__ float opaque_one() {
-  float one = 1.f;
-  asm("" : "+v"(one));
-  return one;
+// one position dominates gets that position's value exactly.
+__device__ __forceinline__ float sum_of(half8 p, float l) {
+  const half2v one = {(f16)1.f, (f16)1.f};
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) l = __builtin_amdgcn_fdot2(half2v{p[e], p[e + 1]}, one, l, false);
+  return l;
 }
 
 template <int D, int QT, bool PAIR, bool SEL>
-__global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendArgs a) {
+__global__ __launch_bounds__(256, QT == 1 ? (PAIR ? 3 : 4) : 2) void k_qcache_attend(AttendArgs a) {
   constexpr int NS = D / 32, NJ = D / 16, CT = 16 * QT;
   constexpr float SLACK = slack_of(PAIR), LIFT = lift_of(PAIR);
   const QCache& c = a.c;
@@ -632,13 +668,24 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
   int vref = 0;
   bool first = true;
 
+  constexpr int LD = D + 4;
+  // the four waves' sums meet in LDS, after each wave's keys of a step
+  // (32 columns: in two rounds, since four waves' sums take more than 64 KB)
+  constexpr int SLOTS = QT == 1 ? 4 : 2;
+  __shared__ __align__(16) float so[SLOTS * CT * LD];
+  __shared__ float sm[4][CT], sl[4][CT];
+  char* keys = (char*)so + wave * (32 * D);
+  static_assert(4 * 32 * D <= sizeof(so));
+
   Step<D> x;
   at.fill();
-  at.next();
+  at.find();
   if (at.ok) {
     load_k<D>(c, at.ph, (at.pos >> 5) & 1, lane, x.k);
     load_v<D>(c, at.ph, (at.pos >> 5) & 1, lane, x.v);
   }
+  at.settle();
+  at.scales();
   // (the first positions are on their way)
   // queries: scaled by a power of two so that a column's largest element is in [2^10, 2^11)
   half8 qh[QT][NS], ql[PAIR ? QT : 1][NS];
@@ -692,13 +739,20 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
         if (PAIR) ql[t][k][e] = (f16)(y - (float)qh[t][k][e]);
       }
   }
-  const float one = opaque_one();
-  // One step; EDGE: some of its positions are masked for a column, or lie behind the row's last one.
-  auto step = [&](auto edge_tag) {
-    constexpr bool EDGE = decltype(edge_tag)::value;
-    const int p0 = at.pos;
-    const float ks = at.ks, vs = at.vs;
-    at.next();  // (the loads of the next step go out as its registers get free)
+  // One step; EDGE: some of its positions are masked for a column, or lie behind the row's last one.  MORE: the next
+  // one's loads go out as its registers get free, without a condition, so that each wait is for what it needs alone.
+  int p0 = 0;
+  float ks = 0.f, vs = 0.f;
+  auto advance = [&] {
+    p0 = at.pos;
+    ks = at.ks;
+    vs = at.vs;
+    at.next();
+  };
+  auto step = [&](auto edge_tag, auto more_tag) {
+    constexpr bool EDGE = decltype(edge_tag)::value, MORE = decltype(more_tag)::value;
+    turn_k<D>(x.k, keys, lane);
+    if (MORE) load_k<D>(c, at.ph, (at.pos >> 5) & 1, lane, x.k);
     // S^T = K Q^T
     f32x4 sc[QT][2];
 #pragma unroll
@@ -707,15 +761,14 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
     for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int k = 0; k < NS; ++k) {
-        const uint4 w = x.k[n][k / 2];
-        const half8 A = k & 1 ? codes_f16(w.z, w.w, 1.f) : codes_f16(w.x, w.y, 1.f);
+        const i32x4 w = *(const i32x4*)(keys + k_slot<D>(16 * n + i, g * (D / 64) + k / 2));
+        const half8 A = k & 1 ? codes_f16(w[2], w[3], 1.f) : codes_f16(w[0], w[1], 1.f);
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           sc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, qh[t][k], sc[t][n], 0, 0, 0);
           if (PAIR) sc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, ql[t][k], sc[t][n], 0, 0, 0);
         }
       }
-    if (at.ok) load_k<D>(c, at.ph, (at.pos >> 5) & 1, lane, x.k);
     // softmax of the 32 positions
     int ve = exponent_of(vs);
     if (first) vref = ve;
@@ -760,10 +813,9 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
           if (PAIR) {
             pl8[t][4 * n + r] = (f16)(p - (float)ph8[t][4 * n + r]);
             l[t] += p;
-          } else {
-            l[t] = fmaf((float)ph8[t][4 * n + r], one, l[t]);
           }
         }
+      if (!PAIR) l[t] = sum_of(ph8[t], l[t]);
     }
     // O^T += V^T P^T; codes behind the row's last position may be anything
     if (EDGE) {
@@ -792,11 +844,14 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
         if (PAIR) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, pl8[t], o[t][j], 0, 0, 0);
       }
     }
-    if (at.ok) load_v<D>(c, at.ph, (at.pos >> 5) & 1, lane, x.v);
+    if (MORE) load_v<D>(c, at.ph, (at.pos >> 5) & 1, lane, x.v);
   };
   // (positions increase, so the steps at the edge are the last ones; vmin <= len)
-  while (at.ok && at.pos + 32 <= vmin) step(std::false_type{});
-  while (at.ok) step(std::true_type{});
+  if (at.ok) {
+    for (advance(); at.ok && p0 + 32 <= vmin; advance()) step(std::false_type{}, std::true_type{});
+    for (; at.ok; advance()) step(std::true_type{}, std::true_type{});
+    step(std::true_type{}, std::false_type{});
+  }
   const float unit = ldexpf(1.f, vref);
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -806,12 +861,6 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
     for (int j = 0; j < NJ; ++j) o[t][j] *= unit;
   }
 
-  constexpr int LD = D + 4;
-  // the four waves' sums meet in LDS
-  // (32 columns: in two rounds, since four waves' sums take more than 64 KB)
-  constexpr int SLOTS = QT == 1 ? 4 : 2;
-  __shared__ __align__(16) float so[SLOTS * CT * LD];
-  __shared__ float sm[4][CT], sl[4][CT];
   const int live = min(ncols - col0, CT);
   if (g == 0)
 #pragma unroll
@@ -828,7 +877,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int j = 0; j < NJ; j += 4)
-            *(f32x4*)&so[(slot * CT + 16 * t + i) * LD + (4 * g + r) * NJ + j] =
+            *(f32x4*)&so[(slot * CT + 16 * t + i) * LD + j * 16 + (4 * g + r) * 4] =
                 f32x4{o[t][j][r], o[t][j + 1][r], o[t][j + 2][r], o[t][j + 3][r]};
   };
 #pragma unroll
@@ -852,7 +901,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_qcache_attend(AttendAr
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) o[t][j][r] += so[(wave * CT + 16 * t + i) * LD + (4 * g + r) * NJ + j];
+            for (int j = 0; j < NJ; ++j) o[t][j][r] += so[(wave * CT + 16 * t + i) * LD + j / 4 * 64 + (4 * g + r) * 4 + j % 4];
     // each of the two waves writes where it alone has read
     if (wave < 2) put(wave);
   }
@@ -924,27 +973,28 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
   const int steps = (vmax + 31) / 32, begin = split * a.per;
   Walk<false> at{c, nullptr, sg.row, h, lane, begin, 1, split == a.splits - 1 ? steps : min(steps, begin + a.per), vmax};
 
-  uint4 kb[D / 32];
+  i32x4 kb[D / 32];
   uint32_t vb[4][NJ];  // of quads f, 2 + f, 4 + f and 6 + f
-  auto load_keys = [&] {
-    const uint8_t* p = c.k + at.ph * (PG * D) + ((at.pos >> 5) & 1) * (32 * D) + i * D + f * (D / 2);
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) kb[e] = *(const uint4*)(p + 16 * e);
-  };
+  __shared__ __align__(16) char turn[4 * 32 * D];
+  char* keys = turn + wave * (32 * D);
+  auto load_keys = [&] { load_k<D>(c, at.ph, (at.pos >> 5) & 1, lane, kb); };
   auto load_values = [&] {
-    const uint8_t* p = c.v + at.ph * (PG * D) + ((at.pos >> 5) & 1) * (32 * D) + f * (4 * D) + i * (4 * NJ);
+    const uint8_t* p = c.v + (at.ph * (PG * D) + ((at.pos >> 5) & 1) * (32 * D));
+    const uint32_t first = f * (4u * D) + i * (4u * NJ);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (NJ == 4) *(uint4*)vb[e] = *(const uint4*)(p + e * 8 * D);
-      else *(uint2*)vb[e] = *(const uint2*)(p + e * 8 * D);
+      if (NJ == 4) *(uint4*)vb[e] = *(const uint4*)(p + first + e * 8 * D);
+      else *(uint2*)vb[e] = *(const uint2*)(p + first + e * 8 * D);
     }
   };
   at.fill();
-  at.next();
+  at.find();
   if (at.ok) {
     load_keys();
     load_values();
   }
+  at.settle();
+  at.scales();
 
   // the query, scaled by a power of two so that its largest element is in [2^10, 2^11)
   const int col = col0 + i;
@@ -1002,24 +1052,30 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
   float m = -INFINITY, l = 0.f;
   int vref = 0;  // o is in units of 2^vref
   bool first = true;
-  const float one = opaque_one();
-  auto step = [&](auto edge_tag) {
-    constexpr bool EDGE = decltype(edge_tag)::value;
-    const int p0 = at.pos;
-    const float cs = fmaxf(cq * at.ks, 1e-37f);  // (not 0: -inf stays -inf)
-    const int ve = exponent_of(at.vs);
+  int p0 = 0;
+  float ks = 0.f, vs = 0.f;
+  auto advance = [&] {
+    p0 = at.pos;
+    ks = at.ks;
+    vs = at.vs;
     at.next();
+  };
+  auto step = [&](auto edge_tag, auto more_tag) {  // as above
+    constexpr bool EDGE = decltype(edge_tag)::value, MORE = decltype(more_tag)::value;
+    const float cs = fmaxf(cq * ks, 1e-37f);  // (not 0: -inf stays -inf)
+    const int ve = exponent_of(vs);
+    turn_k<D>(kb, keys, lane);
+    if (MORE) load_keys();
     f32x16 sc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sc[r] = 0.f;
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
-      const uint4 w = kb[k / 2];
-      const half8 A = k & 1 ? codes_f16(w.z, w.w, 1.f) : codes_f16(w.x, w.y, 1.f);
+      const i32x4 w = *(const i32x4*)(keys + k_slot<D>(i, f * (D / 32) + k / 2));
+      const half8 A = k & 1 ? codes_f16(w[2], w[3], 1.f) : codes_f16(w[0], w[1], 1.f);
       sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, qh[k], sc, 0, 0, 0);
       if (PAIR) sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, ql[k], sc, 0, 0, 0);
     }
-    if (at.ok) load_keys();
     if (first) vref = ve;
     first = false;
     float fall = 1.f;  // o to another unit where the page's scale is far from it
@@ -1053,10 +1109,9 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
       if (PAIR) {
         pl8[r / 8][r % 8] = (f16)(p - (float)ph8[r / 8][r % 8]);
         l += p;
-      } else {
-        l = fmaf((float)ph8[r / 8][r % 8], one, l);
       }
     }
+    if (!PAIR) l = sum_of(ph8[1], sum_of(ph8[0], l));
     if (EDGE) {  // codes behind the row's last position may be anything
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -1074,10 +1129,13 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
         o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, ph8[u], o[j], 0, 0, 0);
         if (PAIR) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, pl8[u], o[j], 0, 0, 0);
       }
-    if (at.ok) load_values();
+    if (MORE) load_values();
   };
-  while (at.ok && at.pos + 32 <= vmin) step(std::false_type{});
-  while (at.ok) step(std::true_type{});
+  if (at.ok) {
+    for (advance(); at.ok && p0 + 32 <= vmin; advance()) step(std::false_type{}, std::true_type{});
+    for (; at.ok; advance()) step(std::true_type{}, std::true_type{});
+    step(std::true_type{}, std::false_type{});
+  }
   l += __shfl_xor(l, 32, 64);
   if (!live) return;
   const float out = a.splits > 1 ? ldexpf(1.f, vref) : l == 0.f ? 0.f : ldexpf(1.f, vref) / l;
@@ -1104,7 +1162,8 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
   }
 }
 
-// Joins the splits of each (token, head): a wave each, in split order.
+// Joins the splits of each (token, head): a wave each, in split order.  (4 rows of 32 heads in about 16 splits: 7 us,
+// all launch and round trips.)
 template <int D>
 __global__ __launch_bounds__(256) void k_qcache_join(AttendArgs a) {
   constexpr int LD = D + 4, E = D / 64;
@@ -1171,13 +1230,16 @@ __global__ __launch_bounds__(256) void k_qcache_join(AttendArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Selection.  A workgroup per KV head and token, or 16 / G of a row's tokens (they read the same bounds).  The score of a page is an upper bound of q . k over
-// its keys, from each channel's largest and smallest key, in whole numbers (|q^| <= 127 times bounds of
-// at most 112, 128 channels: below 2^21), so it has the same bits in any order of summation:
+// Selection.  A workgroup per KV head and token, or 16 / G of a row's tokens (they read the same bounds).  The score of
+// a page is an upper bound of q . k over its keys, from each channel's largest and smallest key, in whole numbers
+// (|q^| <= 127 times bounds of at most 112, 128 channels: below 2^21), so it has the same bits in any order of
+// summation:
 //   2^ke max over heads of sum_d max(q^_d, 0) hi_d + min(q^_d, 0) lo_d
 // as one 8-bit product of [q^+ | q^-] (a head per row) with the bounds [hi | lo] (a page per column).
-// Then the n_sel best, ties to the lower page: up to 1,024 pages by one wave, more by four 8-bit digits of the
-// keys' order.
+// Then the n_sel best, ties to the lower page: a wave finds the key of rank n_sel bit by bit; 257 to 1,024 pages of a
+// single token by eight waves, three bits a round; more than 1,024 by four 8-bit digits.
+// Measured (8 KV heads of 128): 8 tokens over 1,024 pages 17 us, 192 tokens over 125 to 256 pages 14 us, one over 63
+// pages 6.5 us: page table, bounds and ranking wait for each other, and the bytes take less (1,024 pages: 17 MB).
 
 struct SelectArgs {
   QCache c;
