@@ -1238,8 +1238,8 @@ __global__ __launch_bounds__(256) void k_qcache_join(AttendArgs a) {
 // as one 8-bit product of [q^+ | q^-] (a head per row) with the bounds [hi | lo] (a page per column).
 // Then the n_sel best, ties to the lower page: a wave finds the key of rank n_sel bit by bit; 257 to 1,024 pages of a
 // single token by eight waves, three bits a round; more than 1,024 by four 8-bit digits.
-// Measured (8 KV heads of 128): 8 tokens over 1,024 pages 17 us, 192 tokens over 125 to 256 pages 14 us, one over 63
-// pages 6.5 us: page table, bounds and ranking wait for each other, and the bytes take less (1,024 pages: 17 MB).
+// Measured (8 KV heads of 128): 8 tokens over 470 to 1,024 pages 20 us, 192 tokens over 125 to 256 pages 14 us, one
+// over 63 pages 6.6 us: page table, bounds and ranking wait for each other, and the bytes take less (1,024 pages: 17 MB).
 
 struct SelectArgs {
   QCache c;
