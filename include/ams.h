@@ -234,7 +234,8 @@ typedef struct {
  * Values saturate at +-65504.  A token whose key or value of a head holds a NaN
  * gets a NaN key there (every query of that head that sees the token reads NaN;
  * none that does not) and zeros for its NaN values.  Tokens at negative
- * positions are not stored.  A page that a call writes belongs to one row of it.
+ * positions are not stored.  A page that a call writes is the page of one block of
+ * one row (two blocks of a call in one page leave its contents undefined).
  * Errors: AMS_EINVAL, AMS_ENODEV, AMS_EHIP. */
 ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, const int32_t* kv_len, int32_t n_tok,
                              int32_t max_new, const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t dtype,

@@ -34,7 +34,8 @@ class QuantCache:
 
     k [pages, heads, 64, dim] and v [pages, heads, 16, dim, 4] float8_e4m3fn; k_scale, v_scale
     [pages, heads] float32; k_bounds [pages, heads, 2, dim] int8; page_table [rows, pages per row]
-    int32 (entries outside the pool hold no positions).  All contiguous on one device.
+    int32 (entries outside the pool hold no positions).  All contiguous on one device,
+    which is the current one at every call.
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
