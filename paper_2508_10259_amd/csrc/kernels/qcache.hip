@@ -1238,8 +1238,9 @@ __global__ __launch_bounds__(256) void k_qcache_join(AttendArgs a) {
 // as one 8-bit product of [q^+ | q^-] (a head per row) with the bounds [hi | lo] (a page per column).
 // Then the n_sel best, ties to the lower page: a wave finds the key of rank n_sel bit by bit; 257 to 1,024 pages of a
 // single token by eight waves, three bits a round; more than 1,024 by four 8-bit digits.
-// Measured (8 KV heads of 128): 8 tokens over 470 to 1,024 pages 20 us, 192 tokens over 125 to 256 pages 14 us, one
-// over 63 pages 6.6 us: page table, bounds and ranking wait for each other, and the bytes take less (1,024 pages: 17 MB).
+// Measured (8 KV heads of 128): 8 tokens over 470 to 1,024 pages 19 us, 192 tokens over 125 to 256 pages 13 us, one
+// over 63 pages 6.8 us: page table, bounds and ranking wait for each other, on as many CUs as there are tokens and
+// heads (of the 19: 12 for the scores, 0.25 MB a workgroup, and 3 for the ranking).
 
 struct SelectArgs {
   QCache c;
@@ -1307,11 +1308,12 @@ __device__ __forceinline__ void select_all(const QCache& c, int row, int np, int
 template <int D, int NT>
 __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
   // U groups of 16 pages at a time: a wave waits twice (page table, bounds) for all of them
-  constexpr int NW = NT / 64, NB = 2 * D / 64, U = NT == 256 ? 4 : 8;
+  constexpr int NW = NT / 64, NB = 2 * D / 64, U = 4;
   extern __shared__ uint32_t key[];  // [tokens][ppr]
   __shared__ uint32_t hist[256];
   __shared__ uint32_t pick[2];
   __shared__ uint32_t wsum[2][NW];
+  __shared__ i32x4 turn[NW][NB * 64];
   const QCache& c = a.c;
   int id = blockIdx.x;
   const int h = id % c.H;
@@ -1330,31 +1332,41 @@ __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
   const int np = pages_of(nt - 1);
 
   if (np > a.n_sel) {
+    constexpr int PC = D / 8;  // 16-byte pieces of a page's bounds
     int page[U];
     float ks[U];
     i32x4 bound[U][NB];
-    auto fetch_pages = [&](int p0) {
+    auto fetch = [&](int p0) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         page[u] = c.pt[(size_t)sg.row * c.ppr + min(p0 + u * NW * 16 + i, np - 1)];
         page[u] = (unsigned)page[u] < (unsigned)c.n_pages ? page[u] : -1;
       }
-    };
-    auto fetch = [&](auto from, auto to) {
 #pragma unroll
-      for (int u = decltype(from)::value; u < decltype(to)::value; ++u) {
-        const size_t ph = (size_t)max(page[u], 0) * c.H + h;
-        const i32x4* b = (const i32x4*)(c.kb + ph * (2 * D)) + g;
-        ks[u] = c.ks[ph];
+      for (int u = 0; u < U; ++u) {
+        ks[u] = c.ks[(size_t)max(page[u], 0) * c.H + h];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) bound[u][n] = b[4 * n];
+        for (int n = 0; n < NB; ++n) {
+          const size_t ph = (size_t)max(__shfl(page[u], n * (64 / PC) + lane / PC, 64), 0) * c.H + h;
+          bound[u][n] = *((const i32x4*)(c.kb + ph * (2 * D)) + lane % PC);
+        }
       }
     };
-    constexpr std::integral_constant<int, 0> NONE{};
-    constexpr std::integral_constant<int, 4> SOME{};
-    constexpr std::integral_constant<int, U> ALL{};
-    fetch_pages(wave * 16);  // on their way while the queries are (as many as the registers hold beside those)
-    fetch(NONE, SOME);
+    // 16 pages' bounds were loaded as they lie, and are turned in LDS to a page to a lane, as the attention's keys are
+    // (8 tokens over 470 to 1,024 pages, the whole call: 43.2 -> 41.1 us)
+    auto turned = [&](int u) {
+      i32x4* t = turn[wave];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const int row = n * (64 / PC) + lane / PC;
+        t[row * PC + (lane % PC ^ (row & 7))] = bound[u][n];
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int n = 0; n < NB; ++n) bound[u][n] = t[i * PC + ((4 * n + g) ^ (i & 7))];
+    };
+    fetch(wave * 16);  // (on their way while the queries are)
     // Row i of the products: one token's head c0 + i, or, of several tokens, head i % G of token i / G.  Lane (i, g)
     // reads its channels 64 b + 16 g .. of each block b of 64 (all waves the same).
     const int rt = a.toks == 1 ? 0 : i / G;
@@ -1419,14 +1431,10 @@ __global__ __launch_bounds__(NT) void k_qcache_select(SelectArgs a) {
         A[b + D / 64] = dn;
       }
       for (int p0 = wave * 16; p0 < np; p0 += NW * 16 * U) {
-        const bool begun = c0 == 0 && p0 == wave * 16;
-        if (!begun) {
-          fetch_pages(p0);
-          fetch(NONE, SOME);
-        }
-        fetch(SOME, ALL);
+        if (c0 > 0 || p0 != wave * 16) fetch(p0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+          turned(u);
           i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
           for (int n = 0; n < NB; ++n) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(A[n], bound[u][n], acc, 0, 0, 0);
@@ -1637,7 +1645,7 @@ template <int D, int NT>
 static hipError_t select_launch(const SelectArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)a.sg.n_seg * a.c.H * ((a.sg.max_new + a.toks - 1) / a.toks);
   const size_t lds = (size_t)a.toks * a.c.ppr * 4;
-  if (lds > 60 * 1024) {  // above 64 KB with the kernel's own
+  if (lds > 28 * 1024) {  // above 64 KB with the kernel's own
     hipError_t e = hipFuncSetAttribute((const void*)k_qcache_select<D, NT>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)lds);
     if (e != hipSuccess) return e;
