@@ -252,6 +252,24 @@ def test_ragged_long_rows_in_even_pieces(D, G, dtype):
     many.attend((1,) * 70, G, dtype)
 
 
+@pytest.mark.parametrize("D,G,dtype", [(64, 2, "f16"), (128, 1, "f32"), (128, 4, "bf16")])
+@pytest.mark.parametrize("gone", ["scattered", "the last", "all but one"])
+def test_rows_with_pages_missing(D, G, dtype, gone):
+    table = np.arange(160, dtype=np.int32).reshape(2, 80).copy()
+    rng = np.random.default_rng(31)
+    if gone == "scattered":
+        table[:, rng.choice(80, 30, replace=False)] = -1
+    elif gone == "the last":
+        table[0, 70:], table[1, 3:] = -1, 160
+    else:
+        table[0, :40], table[0, 41:], table[1, 1:] = -1, 1 << 29, -7
+    b = Both(2, 80, 1, D, seed=32, table=table, spare=0)
+    b.append((80 * 64 - 60, 75 * 64 + 9), "f16", 1.5)
+    for counts in ((1, 1), (30, 0), (45, 60)):
+        b.attend(counts, G, dtype)
+    b.attend((1, 2), G, dtype, n_select=5)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("stride,shift", [(5, 0), (8, 3), (1, 1)])
 def test_strided_and_unaligned_queries_and_outputs(dtype, stride, shift):
