@@ -228,6 +228,14 @@ __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
     }
   }
   if (page < 0) return;
+  const size_t ph = (size_t)page * c.H + h;
+  // The scales of the page's older positions.  Every wave asks for them before the workgroup's barrier: the first
+  // thread overwrites them at the end, when other waves may only just have left that barrier.
+  float ks_old = 0.f, vs_old = 0.f;
+  if (s0 > 0) {
+    ks_old = c.ks[ph];
+    vs_old = c.vs[ph];
+  }
   // each channel's largest and smallest key (rounding keeps their order, so their codes are the codes' bounds), and
   // the largest |value|
   float hi[8], lo[8], va = 0.f;
@@ -312,10 +320,9 @@ __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
       va = fmaxf(va, red[1][w]);
     }
   }
-  const size_t ph = (size_t)page * c.H + h;
   int ke = scale_exponent(ka), ve = scale_exponent(va), kd = 0, vd = 0;  // kd, vd: older codes' shift (<= 0)
   if (s0 > 0) {
-    const int ko = exponent_of(c.ks[ph]), vo = exponent_of(c.vs[ph]);
+    const int ko = exponent_of(ks_old), vo = exponent_of(vs_old);
     ke = max(ke, ko);
     ve = max(ve, vo);
     kd = ko - ke;

@@ -203,6 +203,19 @@ def test_append_skips_pages_outside_the_pool_and_negative_positions():
     b.check()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [5, 9, 17, 40, 64])
+def test_append_of_many_tokens_to_pages_whose_scale_grows(D, n):
+    """Several waves round a page's older codes again by one scale, which the workgroup replaces meanwhile: the
+    bytes of many pages at once, of every number of older positions."""
+    b = Both(63, 2, 6, D, seed=50 + n + D)
+    b.append(tuple(range(1, 64)), "f16", 0.01)
+    b.append((n,) * 63, "bf16", 50.0)
+    b.check()
+    b.append((min(n, 128 - 63 - n) or 1,) * 63, "f32", 3000.0)
+    b.check()
+
+
 # --- attention ------------------------------------------------------------------------------------
 
 
