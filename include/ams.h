@@ -242,8 +242,9 @@ ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, co
                              void* stream);
 
 /* Bytes of device workspace ams_qcache_attend needs for these sizes, whether it is
- * given `selected` or not (1: none; 0 if an argument is invalid).  Only the
- * dimensions of `cache` are read. */
+ * given `selected` or not (1: none; 0 if an argument is invalid, or the call too
+ * large: ams_qcache_attend takes what needs at most 2^22 workgroups, of 16 to 128
+ * (token, head) pairs of a KV head each).  Only the dimensions of `cache` are read. */
 size_t ams_qcache_workspace_bytes(const ams_qcache* cache, int32_t n_heads, int32_t n_tok, int32_t max_new,
                                   int32_t max_len, int32_t n_select);
 

@@ -118,10 +118,6 @@ struct DevRanges {
   }
 };
 
-// Workgroups of one launch of the 8-bit cache's kernels (of 1,024 threads at most: a grid has fewer than
-// 2^32 threads).
-constexpr int64_t QCACHE_MAX_BLOCKS = (int64_t)1 << 22;
-
 bool aligned256(const void* p) { return ((uintptr_t)p & 255) == 0; }
 
 }  // namespace
@@ -579,6 +575,12 @@ ams::QAttendPlan qcache_plan(const ams_qcache* c, int32_t n_heads, int32_t n_tok
   return ams::qcache_attend_plan(c->rows, n_heads, c->n_kv_heads, c->head_dim, n_tok, std::min(max_new, n_tok),
                                  std::min(max_len, c->pages_per_row * 64), std::min(n_select, c->pages_per_row));
 }
+// Whether the attention's launches stay within their limits: its workgroups, and four (token, head) to a workgroup that
+// joins splits.
+bool qcache_launchable(const ams_qcache* c, const ams::QAttendPlan& p, int32_t n_heads, int32_t max_new) {
+  return p.blocks <= ams::QCACHE_MAX_BLOCKS &&
+         (p.splits == 1 || (int64_t)c->rows * n_heads * max_new <= 4 * ams::QCACHE_MAX_BLOCKS);
+}
 size_t align16(size_t x) { return (x + 15) & ~(size_t)15; }
 
 }  // namespace
@@ -592,7 +594,7 @@ ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, co
     return fail(AMS_EINVAL, e);
   if (n_tok == 0) return AMS_OK;
   max_new = std::min(max_new, n_tok);
-  if (((int64_t)(max_new + 62) / 64 + 1) * cache->n_kv_heads * cache->rows > QCACHE_MAX_BLOCKS)
+  if (((int64_t)(max_new + 62) / 64 + 1) * cache->n_kv_heads * cache->rows > ams::QCACHE_MAX_BLOCKS)
     return fail(AMS_EINVAL, "too many pages for one call: rows * n_kv_heads * max_new / 64 is above 2^22");
   DevRanges in{0};
   if (int s = current_device_again(&in.dev, e)) return fail(s, e);
@@ -612,6 +614,7 @@ size_t ams_qcache_workspace_bytes(const ams_qcache* cache, int32_t n_heads, int3
   if (!qcache_sizes(cache, n_heads, n_tok, max_new, max_len, n_select, e)) return 0;
   if (n_tok == 0) return 1;
   const ams::QAttendPlan p = qcache_plan(cache, n_heads, n_tok, max_new, max_len, n_select);
+  if (!qcache_launchable(cache, p, n_heads, std::min(max_new, n_tok))) return 0;
   return std::max<size_t>(1, align16(p.part_floats * 4) + (size_t)n_tok * cache->n_kv_heads * n_select * 4);
 }
 
@@ -628,8 +631,7 @@ ams_status ams_qcache_attend(const ams_qcache* cache, const int32_t* tok_off, co
   if (n_tok == 0) return AMS_OK;
   const ams::QAttendPlan p = qcache_plan(cache, n_heads, n_tok, max_new, max_len, n_select);
   max_new = std::min(max_new, n_tok);
-  if (p.blocks > QCACHE_MAX_BLOCKS ||
-      (p.splits > 1 && (int64_t)cache->rows * n_heads * max_new > 4 * QCACHE_MAX_BLOCKS))
+  if (!qcache_launchable(cache, p, n_heads, max_new))
     return fail(AMS_EINVAL, "too many queries for one call: rows * n_kv_heads * max_new needs more than 2^22 workgroups");
   const size_t list = (size_t)n_tok * cache->n_kv_heads * n_select * 4, part = align16(p.part_floats * 4);
   const size_t need = part + (selected ? 0 : list);

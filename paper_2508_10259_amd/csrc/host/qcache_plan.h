@@ -11,10 +11,15 @@ namespace ams {
 // A split of an attention has at least this many steps of 32 positions: 8 for each wave that shares it.
 constexpr int QCACHE_LEAST_STEPS = 32;
 
+// Workgroups of one launch of the 8-bit cache's kernels (of 1,024 threads at most: a grid has fewer than
+// 2^32 threads).
+constexpr int64_t QCACHE_MAX_BLOCKS = (int64_t)1 << 22;
+
 // keys: a workgroup's four waves share qt tiles of 16 query columns and deal the positions among them;
 // otherwise each wave has qt tiles of its own.  tiles: workgroups along a segment's columns; splits: at most
 // as many along its positions, `per` steps of 32 each (even: as many as make the pieces of all segments equal),
-// leaving partial sums of part_floats in all (0 for one split).
+// leaving partial sums of part_floats in all (0 for one split).  blocks above 2^31 - 1: no launch can
+// hold them, and nothing else is planned.
 struct QAttendPlan {
   bool keys, even;
   int qt, tiles, splits, per;
@@ -31,10 +36,13 @@ inline QAttendPlan qcache_attend_plan(int n_seg, int n_heads, int n_kv, int dh, 
   p.keys = n_select > 0 || cols <= 32;
   p.qt = p.keys && (cols <= 16 || n_select) ? 1 : 2;
   const int width = p.keys ? 16 * p.qt : 64 * p.qt;
-  p.tiles = (int)((cols + width - 1) / width);
+  const int64_t tiles = (cols + width - 1) / width;
+  const int64_t blocks = (int64_t)n_seg * n_kv * tiles * (n_select ? max_new : 1);  // (below 2^62 by the calls' limits)
+  p.blocks = blocks;
+  if (blocks > INT32_MAX) return p;
+  p.tiles = (int)tiles;
   // Splits are for launches with too few workgroups; joining them costs a launch (4 us) and a round trip
   // through memory (16 rows of 600 to 656 positions in fp32, 32 heads of 128: 19.5 us in one split, 28 in two).
-  const int64_t blocks = (int64_t)n_seg * n_kv * p.tiles * (n_select ? max_new : 1);
   const int64_t steps = (n_select ? (int64_t)n_select * 64 : max_len) / 32 + 1;
   const size_t one = (size_t)n_tok * n_heads * (dh + 4);
   const int64_t fit = (int64_t)std::min<size_t>(room / one, 512);

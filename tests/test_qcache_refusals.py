@@ -73,6 +73,16 @@ def test_too_large_a_launch(lib):
     assert _attend(lib, c, n_tok=1 << 30, max_new=1 << 20, n_heads=1024) == -1
 
 
+@pytest.mark.parametrize("n_tok", [1 << 23, (1 << 23) + 1, (1 << 31) - 1])
+@pytest.mark.parametrize("n_select", [0, 1])
+def test_more_queries_than_an_int_counts_tiles(lib, n_tok, n_select):
+    """65,536 heads on one KV head: 2^32 tiles of 128 queries and more."""
+    c = _cache(n_kv_heads=1, head_dim=128, rows=1)
+    assert lib.ams_qcache_workspace_bytes(C.byref(c), 65536, n_tok, n_tok, 100, n_select) == 0
+    assert _attend(lib, c, n_tok=n_tok, max_new=n_tok, n_heads=65536, ldq=1 << 23, ldo=1 << 23, n_select=n_select,
+                   ws_bytes=1 << 62) == -1
+
+
 def test_workspace_grows_with_splits_and_lists(lib):
     c = _cache(rows=1, pages_per_row=4096)
     one = lib.ams_qcache_workspace_bytes(C.byref(c), 4, 1, 1, 64, 0)
