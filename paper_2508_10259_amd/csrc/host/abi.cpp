@@ -594,7 +594,7 @@ ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, co
     return fail(AMS_EINVAL, e);
   if (n_tok == 0) return AMS_OK;
   max_new = std::min(max_new, n_tok);
-  if (((int64_t)(max_new + 62) / 64 + 1) * cache->n_kv_heads * cache->rows > ams::QCACHE_MAX_BLOCKS)
+  if ((((int64_t)max_new + 62) / 64 + 1) * cache->n_kv_heads * cache->rows > ams::QCACHE_MAX_BLOCKS)
     return fail(AMS_EINVAL, "too many pages for one call: rows * n_kv_heads * max_new / 64 is above 2^22");
   DevRanges in{0};
   if (int s = current_device_again(&in.dev, e)) return fail(s, e);

@@ -83,6 +83,13 @@ def test_more_queries_than_an_int_counts_tiles(lib, n_tok, n_select):
                    ws_bytes=1 << 62) == -1
 
 
+@pytest.mark.parametrize("n_tok", [(1 << 31) - 63, (1 << 31) - 62, (1 << 31) - 1])
+def test_append_of_as_many_tokens_as_an_int_holds(lib, n_tok):
+    c = _cache(n_kv_heads=1, rows=1)
+    assert _append(lib, c, n_tok=n_tok, max_new=n_tok, ldk=64, ldv=64) == -1
+    assert b"too many pages" in lib.ams_last_error()
+
+
 def test_workspace_grows_with_splits_and_lists(lib):
     c = _cache(rows=1, pages_per_row=4096)
     one = lib.ams_qcache_workspace_bytes(C.byref(c), 4, 1, 1, 64, 0)
