@@ -531,10 +531,15 @@ bool qcache_type(int32_t dtype, std::string& e) {
   return false;
 }
 
-// A [n_tok][heads][head_dim] tensor with a token stride of ld elements.
-bool qcache_tensor(const void* p, int64_t ld, int32_t n_tok, int64_t width, int32_t dtype, DevRanges& in,
-                   const char* what, std::string& e) {
+// A [n_tok][heads][head_dim] tensor with a token stride of ld elements: its stride and alignment (no device is asked), and
+// its bytes from the first element to the last.
+bool qcache_tensor(const void* p, int64_t ld, int32_t n_tok, int64_t width, int32_t dtype, const char* what, size_t* bytes,
+                   std::string& e) {
   const int64_t es = dtype == AMS_F32 ? 4 : 2;
+  if (!p) {
+    e = std::string(what) + " is NULL";
+    return false;
+  }
   if (ld < width || ld > ((int64_t)1 << 40)) {
     e = std::string(what) + ": token stride must be at least heads * head_dim (and at most 2^40) elements";
     return false;
@@ -543,10 +548,16 @@ bool qcache_tensor(const void* p, int64_t ld, int32_t n_tok, int64_t width, int3
     e = std::string(what) + " is not aligned to its type";
     return false;
   }
-  return in(p, (size_t)(((int64_t)(n_tok - 1) * ld + width) * es), what, e);
+  *bytes = (size_t)(((int64_t)(n_tok - 1) * ld + width) * es);
+  return true;
 }
 
-bool qcache_arrays(const ams_qcache* c, const int32_t* tok_off, const int32_t* kv_len, DevRanges& in, std::string& e) {
+// The cache's arrays and the call's offsets and lengths: there, and aligned (no device is asked).
+bool qcache_aligned(const ams_qcache* c, const int32_t* tok_off, const int32_t* kv_len, std::string& e) {
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->k_bounds || !c->page_table || !tok_off || !kv_len) {
+    e = "the cache's arrays, tok_off and kv_len must not be NULL";
+    return false;
+  }
   if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->k_bounds) & 15) {
     e = "the cache's k, v and k_bounds must be 16-byte aligned";
     return false;
@@ -556,6 +567,10 @@ bool qcache_arrays(const ams_qcache* c, const int32_t* tok_off, const int32_t* k
     e = "scales, page_table, tok_off and kv_len must be 4-byte aligned";
     return false;
   }
+  return true;
+}
+
+bool qcache_arrays(const ams_qcache* c, const int32_t* tok_off, const int32_t* kv_len, DevRanges& in, std::string& e) {
   const size_t ph = (size_t)c->n_pages * c->n_kv_heads, d = c->head_dim;
   return in(c->k, ph * 64 * d, "cache k", e) && in(c->v, ph * 64 * d, "cache v", e) &&
          in(c->k_scale, ph * 4, "cache k_scale", e) && in(c->v_scale, ph * 4, "cache v_scale", e) &&
@@ -596,11 +611,14 @@ ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, co
   max_new = std::min(max_new, n_tok);
   if ((((int64_t)max_new + 62) / 64 + 1) * cache->n_kv_heads * cache->rows > ams::QCACHE_MAX_BLOCKS)
     return fail(AMS_EINVAL, "too many pages for one call: rows * n_kv_heads * max_new / 64 is above 2^22");
+  const int64_t width = (int64_t)cache->n_kv_heads * cache->head_dim;
+  size_t k_bytes, v_bytes;
+  if (!qcache_aligned(cache, tok_off, kv_len, e) || !qcache_tensor(k, ldk, n_tok, width, dtype, "k", &k_bytes, e) ||
+      !qcache_tensor(v, ldv, n_tok, width, dtype, "v", &v_bytes, e))
+    return fail(AMS_EINVAL, e);
   DevRanges in{0};
   if (int s = current_device_again(&in.dev, e)) return fail(s, e);
-  const int64_t width = (int64_t)cache->n_kv_heads * cache->head_dim;
-  if (!qcache_arrays(cache, tok_off, kv_len, in, e) || !qcache_tensor(k, ldk, n_tok, width, dtype, in, "k", e) ||
-      !qcache_tensor(v, ldv, n_tok, width, dtype, in, "v", e))
+  if (!qcache_arrays(cache, tok_off, kv_len, in, e) || !in(k, k_bytes, "k", e) || !in(v, v_bytes, "v", e))
     return fail(AMS_EINVAL, e);
   const ams::QSegs sg{nullptr, tok_off, nullptr, kv_len, 0, cache->rows, n_tok, max_new};
   hipError_t r = ams::qcache_append(qcache_view(cache), sg, k, ldk, v, ldv, dtype, nullptr, (hipStream_t)stream);
@@ -639,11 +657,14 @@ ams_status ams_qcache_attend(const ams_qcache* cache, const int32_t* tok_off, co
   if ((uintptr_t)ws & 15) return fail(AMS_EINVAL, "ws must be 16-byte aligned");
   if (ws_bytes < need) return fail(AMS_ENOMEM, "workspace too small: need " + std::to_string(need));
   if ((uintptr_t)selected & 3) return fail(AMS_EINVAL, "selected must be 4-byte aligned");
+  const int64_t width = (int64_t)n_heads * cache->head_dim;
+  size_t q_bytes, out_bytes;
+  if (!qcache_aligned(cache, tok_off, kv_len, e) || !qcache_tensor(q, ldq, n_tok, width, dtype, "q", &q_bytes, e) ||
+      !qcache_tensor(out, ldo, n_tok, width, dtype, "out", &out_bytes, e))
+    return fail(AMS_EINVAL, e);
   DevRanges in{0};
   if (int s = current_device_again(&in.dev, e)) return fail(s, e);
-  const int64_t width = (int64_t)n_heads * cache->head_dim;
-  if (!qcache_arrays(cache, tok_off, kv_len, in, e) || !qcache_tensor(q, ldq, n_tok, width, dtype, in, "q", e) ||
-      !qcache_tensor(out, ldo, n_tok, width, dtype, in, "out", e) ||
+  if (!qcache_arrays(cache, tok_off, kv_len, in, e) || !in(q, q_bytes, "q", e) || !in(out, out_bytes, "out", e) ||
       (need && !in(ws, need, "ws", e)) || (selected && !in(selected, list, "selected", e)))
     return fail(AMS_EINVAL, e);
   const ams::QCache c = qcache_view(cache);

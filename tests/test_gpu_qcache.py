@@ -542,3 +542,55 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
     del big
     torch.cuda.empty_cache()
+
+
+def test_arrays_that_end_too_early_or_lie_on_the_host_are_refused():
+    """Each array of a call in turn: sizes that no allocation here has, and host memory.  Nothing is launched."""
+    import ctypes as C
+    import torch
+    from paper_2508_10259_amd import capi
+    b = Both(2, 2, 2, 64, seed=45)
+    b.append((5, 3), "f16")
+    q, _ = b.tokens((1, 1), 4, "f16")
+    kv, _ = b.tokens((1, 1), 2, "f16")
+    off, lens = b.where((1, 1))
+    out, ws = torch.full_like(q, 3.0), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    host, lib = torch.zeros(1 << 16, dtype=torch.uint8), b.dev.lib
+    torch.cuda.synchronize()
+    before = [t.view(torch.uint8).clone() for t in (b.dev.k, b.dev.v, b.dev.k_scale, b.dev.v_scale, b.dev.k_bounds)]
+
+    def both(want=capi.AMS_EINVAL, which="append attend", n_tok=2, max_len=8, n_select=0, selected=None, **kw):
+        c = capi.QCache.from_buffer_copy(b.dev.c)
+        p = dict(tok_off=off.data_ptr(), kv_len=lens.data_ptr(), k=kv.data_ptr(), v=kv.data_ptr(), q=q.data_ptr(),
+                 out=out.data_ptr(), ws=ws.data_ptr(), ld=256, ws_bytes=1 << 40)
+        for name, x in kw.items():
+            if name in p:
+                p[name] = x
+            else:
+                setattr(c, name[6:] if name.startswith("cache_") else name, x)
+        got = []
+        if "append" in which:
+            got.append(lib.ams_qcache_append(C.byref(c), p["tok_off"], p["kv_len"], n_tok, 1, p["k"], max(p["ld"], 128), p["v"],
+                                             max(p["ld"], 128), capi.AMS_F16, None))
+        if "attend" in which:
+            got.append(lib.ams_qcache_attend(C.byref(c), p["tok_off"], p["kv_len"], n_tok, 1, max_len, 4, p["q"], p["ld"],
+                                             p["out"], p["ld"], capi.AMS_F16, 0.1, n_select, selected, p["ws"], p["ws_bytes"], None))
+        assert got == [want] * len(got), (kw, got, lib.ams_last_error())
+    h = host.data_ptr() // 16 * 16 + 16
+    for name in ("k", "v", "k_scale", "v_scale", "k_bounds", "page_table"):
+        both(**{"cache_" + name: h})
+    for name in ("tok_off", "kv_len"):
+        both(**{name: h})
+    for name, which in (("k", "append"), ("v", "append"), ("q", "attend"), ("out", "attend")):
+        both(which=which, **{name: h})
+    both(n_pages=1 << 28)
+    both(rows=65535, pages_per_row=16384)
+    both(ld=1 << 38)
+    both(n_tok=1 << 30)
+    both(which="attend", n_select=2, selected=h)
+    both(which="attend", n_select=2, ws=h)
+    both(which="attend", n_select=16384, n_tok=1 << 14, ld=256)
+    torch.cuda.synchronize()
+    assert bool((out == 3).all())
+    for t, x in zip((b.dev.k, b.dev.v, b.dev.k_scale, b.dev.v_scale, b.dev.k_bounds), before):
+        assert torch.equal(t.view(torch.uint8), x)

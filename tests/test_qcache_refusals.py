@@ -90,6 +90,40 @@ def test_append_of_as_many_tokens_as_an_int_holds(lib, n_tok):
     assert b"too many pages" in lib.ams_last_error()
 
 
+ARRAYS = [(n, None) for n in ("k", "v", "k_scale", "v_scale", "k_bounds", "page_table", "tok_off", "kv_len")] + \
+    [(n, 4096 + x) for n in ("k", "v", "k_bounds") for x in (1, 4, 8)] + \
+    [(n, 4096 + x) for n in ("k_scale", "v_scale", "page_table", "tok_off", "kv_len") for x in (1, 2)]
+
+
+@pytest.mark.parametrize("name,at", ARRAYS)
+def test_arrays_missing_or_misaligned(lib, name, at):
+    call = dict(tok_off=64, kv_len=64)
+    c = _cache(**({} if name in call else {name: at}))
+    if name in call:
+        call[name] = at
+    off, lens = call["tok_off"], call["kv_len"]
+    assert lib.ams_qcache_append(C.byref(c), off, lens, 4, 2, 4096, 128, 4096, 128, 2, None) == -1
+    assert lib.ams_qcache_attend(C.byref(c), off, lens, 4, 2, 100, 4, 4096, 256, 4096, 256, 2, 0.1, 0, None, 4096, 1 << 30,
+                                 None) == -1
+
+
+@pytest.mark.parametrize("dtype,es", [(0, 4), (1, 2), (2, 2)])
+def test_tensors_missing_misaligned_or_overlapping_their_next_token(lib, dtype, es):
+    c = _cache()
+
+    def append(k=4096, v=4096, ldk=128, ldv=128):
+        return lib.ams_qcache_append(C.byref(c), 64, 64, 4, 2, k, ldk, v, ldv, dtype, None)
+
+    def attend(q=4096, out=4096, ldq=256, ldo=256):
+        return lib.ams_qcache_attend(C.byref(c), 64, 64, 4, 2, 100, 4, q, ldq, out, ldo, dtype, 0.1, 0, None, 4096, 1 << 30, None)
+    for bad in (None, 4096 + es // 2, 4096 + es + 1):
+        assert append(k=bad) == append(v=bad) == attend(q=bad) == attend(out=bad) == -1
+    for bad in (0, -128, 127, (1 << 40) + 1):
+        assert append(ldk=bad) == append(ldv=bad) == -1
+    for bad in (0, -256, 255, (1 << 40) + 1):
+        assert attend(ldq=bad) == attend(ldo=bad) == -1
+
+
 def test_workspace_grows_with_splits_and_lists(lib):
     c = _cache(rows=1, pages_per_row=4096)
     one = lib.ams_qcache_workspace_bytes(C.byref(c), 4, 1, 1, 64, 0)
