@@ -548,6 +548,11 @@ bool qcache_tensor(const void* p, int64_t ld, int32_t n_tok, int64_t width, int3
     e = std::string(what) + " is not aligned to its type";
     return false;
   }
+  // ((n_tok - 1) * ld + width) * es, of up to 2^31 tokens 2^40 elements apart
+  if (n_tok - 1 > (INT64_MAX / es - width) / ld) {
+    e = std::string(what) + " would take more than 2^63 bytes";
+    return false;
+  }
   *bytes = (size_t)(((int64_t)(n_tok - 1) * ld + width) * es);
   return true;
 }

@@ -124,6 +124,21 @@ def test_tensors_missing_misaligned_or_overlapping_their_next_token(lib, dtype, 
         assert attend(ldq=bad) == attend(ldo=bad) == -1
 
 
+@pytest.mark.parametrize("dtype,es", [(0, 4), (1, 2), (2, 2)])
+def test_tensors_whose_bytes_64_bits_do_not_count(lib, dtype, es):
+    """2^40 elements between tokens: 2^63 bytes and a little, and four times as many, which once counted as one token's."""
+    c = _cache(n_pages=1, n_kv_heads=1, rows=1)
+    for bits in (63, 65):
+        a = dict(n_tok=(1 << (bits - 40)) // es + 1, max_new=1, dtype=dtype)
+        big = 1 << 40
+        assert _append(lib, c, ldk=big, ldv=64, **a) == _append(lib, c, ldk=64, ldv=big, **a) == -1
+        assert b"2^63 bytes" in lib.ams_last_error()
+        for n_select in (0, 1):
+            for ldq, ldo in ((big, 64), (64, big)):
+                assert _attend(lib, c, n_heads=1, ldq=ldq, ldo=ldo, n_select=n_select, **a) == -1
+                assert b"2^63 bytes" in lib.ams_last_error()
+
+
 def test_workspace_grows_with_splits_and_lists(lib):
     c = _cache(rows=1, pages_per_row=4096)
     one = lib.ams_qcache_workspace_bytes(C.byref(c), 4, 1, 1, 64, 0)
