@@ -300,6 +300,17 @@ def test_scores_from_nothing_to_one_position_taking_all(scale, std):
     b.attend((1, 3), 2, "f16", scale=scale, std=std)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("scale,std", [(1.0, 2.0 ** 12), (64.0, 2.0 ** 12), (512.0, 2.0 ** 13), (2.0 ** 14, 2.0 ** 13), (1e12, 1.0), (1e25, 100.0)])
+@pytest.mark.parametrize("G,n_select", [(2, 0), (40, 0), (3, 2)])
+def test_scores_far_beyond_what_an_exponential_tells_apart(dtype, scale, std, G, n_select):
+    """Scores of 2^25 and more, where one position takes all: neighbouring fp32 values are further apart than fp16
+    exponentials reach, and every output is that position's value all the same."""
+    b = Both(2, 3, 1, 64, seed=5)
+    b.append((130, 64), "f32", 2000.0)
+    b.attend((1, 3), G, dtype, scale=scale, std=std, n_select=n_select)
+
+
 def test_pages_of_very_different_scales():
     b = Both(1, 8, 1, 64, seed=11)
     for std in (1e-8, 1.0, 3000.0, 1e-3, 50.0, 1e-9, 1.0):
