@@ -241,8 +241,8 @@ ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, co
                              int32_t max_new, const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t dtype,
                              void* stream);
 
-/* Bytes of device workspace ams_qcache_attend needs for these sizes, whether it is
- * given `selected` or not (1: none; 0 if an argument is invalid, or the call too
+/* Bytes of device workspace ams_qcache_attend needs for these sizes, 4 * n_tok *
+ * n_kv_heads * n_select fewer where it is given `selected` (1: none; 0 if an argument is invalid, or the call too
  * large: ams_qcache_attend takes what needs at most 2^22 workgroups, of 16 to 128
  * (token, head) pairs of a KV head each).  Only the dimensions of `cache` are read. */
 size_t ams_qcache_workspace_bytes(const ams_qcache* cache, int32_t n_heads, int32_t n_tok, int32_t max_new,

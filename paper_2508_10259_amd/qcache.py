@@ -146,6 +146,8 @@ class QuantCache:
         if max_len is None:
             max_len = self.c.pages_per_row * PAGE
         ws, need = None, self._workspace(self._ref, heads, n, max_new, max_len, n_select)
+        if need and selected is not None:
+            need -= 4 * selected.numel()  # (the size counts a list of the pages chosen, which has a place of its own here)
         if need > 1:
             # from the allocator at every call: its memory follows the stream, and a captured graph's stays with it
             ws = torch.empty(need, dtype=torch.uint8, device=self.device)

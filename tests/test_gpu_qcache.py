@@ -446,6 +446,28 @@ def test_arrays_cut_out_of_stacks_of_layers():
     b.attend((1, 3), 2, "bf16", n_select=1)
 
 
+@pytest.mark.parametrize("rows", [1, 40])
+def test_one_list_of_selected_pages_is_allocated(rows):
+    """Beside the caller's list of pages and the output, a call takes the partial sums of its splits and no second list."""
+    import torch
+    b = Both(rows, 3, 4, 64, seed=28)
+    b.append((150,) * rows, "f16")
+    q, _ = b.tokens((3,) * rows, 8, "f16")
+    off, lens = b.where((3,) * rows)
+    selected = torch.empty(3 * rows, 4, 16384, dtype=torch.int32, device="cuda")
+    for given in (selected, None):
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        got = b.dev.attend_selected(q, off, lens, 16384, max_new=3, max_len=192, selected=given)
+        parts = 4 * 3 * rows * 8 * 68 * 32  # floats of 32 splits, more than three pages have
+        most = q.numel() * 2 + parts + (0 if given is not None else 4 * selected.numel()) + 4096
+        assert torch.cuda.max_memory_allocated() - before <= most < 4 * selected.numel() * (2 if given is None else 1)
+        torch.cuda.synchronize()
+        assert got[1].cpu()[:, :, :4].tolist() == [[[0, 1, 2, -1]] * 4] * (3 * rows)
+        del got
+
+
 # --- together -------------------------------------------------------------------------------------
 
 
