@@ -200,7 +200,8 @@ ams_status ams_index_hash_noalloc(const void* data, size_t n_bytes, int32_t seg_
  *            its value times its page's scale
  *   k_bounds int8 [n_pages][n_kv_heads][2][head_dim]: per channel the largest
  *            ceil(key / 4), then the smallest floor(key / 4) over the page's
- *            positions, in units of the scale (what a selection of pages reads)
+ *            positions, in units of the scale (what a selection of pages reads);
+ *            -128 and 127 for a channel that holds NaN only
  *   page_table  int32 [rows][pages_per_row]: the page of each row's 64-position
  *            block; entries outside [0, n_pages) hold no positions (an append
  *            skips them, an attention does not see them).

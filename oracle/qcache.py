@@ -100,8 +100,10 @@ def append(c: Cache, row: int, p0: int, k: np.ndarray, v: np.ndarray) -> None:
                     hi = np.where(np.isnan(val).all(0), -128, np.ceil(np.nanmax(np.where(np.isnan(val), -1e9, val), 0) / 4))
                     lo = np.where(np.isnan(val).all(0), 127, np.floor(np.nanmin(np.where(np.isnan(val), 1e9, val), 0) / 4))
                     if s0 > 0:
-                        hi = np.maximum(hi, np.ceil(c.bounds[page, h, 0] * 2.0 ** shift))
-                        lo = np.minimum(lo, np.floor(c.bounds[page, h, 1] * 2.0 ** shift))
+                        up, down = c.bounds[page, h]
+                        some = up != -128  # a channel that held NaN only had no bounds
+                        hi = np.where(some, np.maximum(hi, np.ceil(up * 2.0 ** shift)), hi)
+                        lo = np.where(some, np.minimum(lo, np.floor(down * 2.0 ** shift)), lo)
                     c.bounds[page, h] = np.stack([hi, lo])
                 else:
                     c.v[page, h] = codes.reshape(PAGE // 4, 4, D).transpose(0, 2, 1)

@@ -404,7 +404,7 @@ __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
       const uint32_t w = pack_codes(some ? hi[e] * ki : 0.f, some ? lo[e] * ki : 0.f, 0.f, 0.f);
       float nh = some ? ceilf(__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * 0.25f) : -128.f;
       float nl = some ? floorf(__builtin_amdgcn_cvt_f32_fp8((int)w, 1) * 0.25f) : 127.f;
-      if (s0 > 0) {
+      if (s0 > 0 && bh[e] != -128) {  // (-128: NaN only so far, a bound that does not move with the scale)
         nh = fmaxf(nh, ceilf(ldexpf((float)bh[e], kd)));
         nl = fminf(nl, floorf(ldexpf((float)bl[e], kd)));
       }

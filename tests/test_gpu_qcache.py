@@ -216,6 +216,29 @@ def test_append_of_many_tokens_to_pages_whose_scale_grows(D, n):
     b.check()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("counts", [(1, 1), (2, 30), (40, 1), (20, 44)])
+def test_bounds_of_pages_that_began_with_nan(D, counts):
+    """The bounds are those of the keys there are, though the scale of the NaN tokens was another."""
+    b = Both(3, 2, 2, D, seed=52)
+
+    def nan(t, t64, value=False):
+        if not value:
+            t[:, :, 1:4], t64[:, :, 1:4] = float("nan"), float("nan")
+
+    def low(t, t64, value=False):
+        t.sub_(1000.0)
+        t64[:] = t.double().cpu().numpy()
+    b.append((counts[0],) * 3, "f16", 0.01, edit=nan)
+    b.check()
+    b.append((counts[1],) * 3, "f32", 100.0, edit=low)
+    b.check()
+    K = Q.VALUES[b.ref.k[b.ref.table[:, 0], :, :sum(counts)]]
+    got = b.dev.k_bounds.cpu().numpy()[b.ref.table[:, 0]]
+    assert np.array_equal(got[:, :, 0, 1:4], np.ceil(np.nanmax(K, 2) / 4)[:, :, 1:4])
+    assert np.array_equal(got[:, :, 1, 1:4], np.floor(np.nanmin(K, 2) / 4)[:, :, 1:4])
+
+
 # --- attention ------------------------------------------------------------------------------------
 
 

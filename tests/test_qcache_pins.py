@@ -60,6 +60,20 @@ def test_bounds_hold_over_many_appends():
         assert np.all(K <= 4 * c.bounds[lp, 0, 0]) and np.all(K >= 4 * c.bounds[lp, 0, 1])
 
 
+def test_bounds_of_a_page_that_began_with_nan():
+    """NaN tokens leave no bounds behind, whatever the scale does afterwards."""
+    c = _empty()
+    x = np.full((2, 1, 8), 0.25)
+    x[:, 0, :3] = np.nan
+    Q.append(c, 0, 0, x, x)
+    assert c.bounds[0, 0, :, 0].tolist() == [-128, 127]
+    y = -np.abs(np.random.default_rng(8).normal(size=(3, 1, 8)) * 300) - 1000
+    Q.append(c, 0, 2, y, y)
+    K = Q.VALUES[c.k[0, 0, :5]]
+    assert np.array_equal(c.bounds[0, 0, 0], np.ceil(np.nanmax(K, 0) / 4))
+    assert np.array_equal(c.bounds[0, 0, 1], np.floor(np.nanmin(K, 0) / 4))
+
+
 def test_nan_reaches_those_who_see_it_only():
     c = _empty()
     x = np.random.default_rng(4).normal(size=(10, 1, 8))
