@@ -11,11 +11,12 @@ import oracle.qcache as Q
 class QuantRow:
     """Steps with given fed-back bins; `select`: pages that a decode query attends to (0: all).
 
-    margin: the smallest relative gap met between the last chosen page's score and the first one left out.
+    margin: the smallest relative gap met between the last chosen page's score and the first one left out;
+    units: the same gap in whole numbers of the score (of the largest key scale among the row's pages).
     """
 
     def __init__(self, p, capacity, select=0):
-        self.p, self.select, self.margin = p, select, math.inf
+        self.p, self.select, self.margin, self.units = p, select, math.inf, math.inf
         c = p.cfg
         n = capacity // 64
         z = lambda *s: np.zeros((n, c.n_heads) + s, np.uint8)  # noqa: E731
@@ -57,6 +58,7 @@ class QuantRow:
         kept, left = [s[i] for i in pages if i < n - 1], [s[i] for i in range(n - 1) if i not in pages]
         if kept and left:
             self.margin = min(self.margin, (min(kept) - max(left)) / max(map(abs, s)))
+            self.units = min(self.units, (min(kept) - max(left)) * 2.0 ** -int(cache.ke[:n, head].max()))
 
     def commit(self, x):
         if x is not None and len(x):

@@ -334,6 +334,46 @@ def test_scores_far_beyond_what_an_exponential_tells_apart(dtype, scale, std, G,
     b.attend((1, 3), G, dtype, scale=scale, std=std, n_select=n_select)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("bits", [16, 20, 24, 28])
+@pytest.mark.parametrize("new", [1, 40])
+def test_a_long_tail_under_one_large_score(dtype, bits, new):
+    """One position whose value is 0 and whose weight is 2^bits times any other's: the outputs are the tail's.
+    Its probabilities may be subnormal fp16, off by half a step, 2^-25, where the largest is 2^4 or more (fp32
+    queries: 2^-25 where it is 2^12)."""
+    import torch
+    n, D = 6000, 64
+    b = Both(1, 95, 1, D, seed=29)
+    at, big = 17, 128.0
+
+    def edit(t, t64, value=False):
+        if value:
+            t64 += 1.0
+            t64[at] = 0.0
+        else:
+            t64[:] = 0.0
+            t64[at, :, 0] = big
+        t.copy_(torch.from_numpy(t64))
+        t64[:] = t.double().cpu().numpy()
+    b.append((n,), "f32", edit=edit)
+    q = torch.zeros(new, 1, D, device="cuda", dtype=dtype_of(dtype))
+    q[:, 0, 0] = bits / 8
+    off, lens = b.where((new,))
+    got = b.dev.attend(q, off, lens, max_new=new, max_len=n, scale=math.log(2.0) * 8 / big)
+    got = got.double().cpu().numpy()[:, 0]
+    for i in range(new):
+        vis = n - new + 1 + i
+        want, size, score = Q.attend(b.ref, 0, 0, q[i].double().cpu().numpy(), vis, math.log(2.0) * 8 / big)
+        _, V, _ = Q.keys_values(b.ref, 0, 0, range(-(-vis // 64)))
+        # the terms of `compare`, and the subnormals' (a weight is a probability over a sum of at least the largest one)
+        p = 2.0 ** -22 if dtype == "f32" else 2.0 ** -11
+        tol = HALF_STEP[dtype] * np.abs(want) + size * (
+            p + 2 * score * (D + 8) * 2.0 ** -24 + 2 * vis * 2.0 ** -24 + 4 * 2.0 ** -23)
+        tol = tol + np.abs(V[:vis]).sum(0) * 2.0 ** -25 / 2.0 ** (12 if dtype == "f32" else 4)
+        assert np.all(np.abs(got[i] - want[0]) <= tol[0] * (1 + HALF_STEP[dtype])), float((np.abs(got[i] - want[0]) / tol[0]).max())
+        assert np.all(np.abs(want[0]) > 0)
+
+
 def test_pages_of_very_different_scales():
     b = Both(1, 8, 1, 64, seed=11)
     for std in (1e-8, 1.0, 3000.0, 1e-3, 50.0, 1e-9, 1.0):
@@ -541,6 +581,51 @@ def test_a_decode_loop_in_a_graph_follows_its_lengths(n_select):
         other = Both(2, 2, H, D, seed=100 + r)
         other.append((70, 3), "f16")
         other.attend((1, 2), G, "f16", n_select=n_select)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_two_graphs_replayed_in_turn(dtype):
+    """Two captured decode steps of two caches, both with workspaces of their own (splits, and a selection), replayed in
+    turn with eager calls between them: every replay gives the eager call's bits."""
+    import torch
+    H, G, D, ppr = 1, 2, 64, 40
+    cache, steps, graphs, outs = [], [], [], []
+    for n in range(2):
+        b = Both(2, ppr, H, D, seed=47 + n)
+        b.append((1900 + 300 * n, 700), "f16")
+        q, _ = b.tokens((1, 1), H * G, dtype)
+        off, lens = b.where((1, 1))
+        cache.append((b, q))
+
+        def step(b=b, q=q, off=off, lens=lens):
+            return (b.dev.attend(q, off, lens, max_new=1, max_len=ppr * 64),
+                    *b.dev.attend_selected(q, off, lens, 20, max_new=1, max_len=ppr * 64))
+        steps.append(step)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for step in steps:
+            step()
+    torch.cuda.synchronize()
+    for step in steps:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step())
+        graphs.append(g)
+    rng = np.random.default_rng(3)
+    for r in range(5):
+        for b, q in cache:
+            q.copy_(torch.from_numpy(rng.normal(size=tuple(q.shape))))
+        torch.cuda.synchronize()
+        for g in graphs if r % 2 else graphs[::-1]:
+            g.replay()
+            if r == 3:
+                steps[0]()  # eager work of one of the caches between the replays
+        got = [[t.clone() for t in o] for o in outs]
+        torch.cuda.synchronize()
+        for step, g in zip(steps, got):
+            for x, y in zip(step(), g):
+                assert torch.equal(x, y)
 
 
 def test_two_streams_and_repeated_calls_give_the_same_bits():

@@ -126,6 +126,40 @@ def test_selected_pages_of_a_decode():
     ctx.close()
 
 
+def test_selected_pages_that_no_rounding_exchanges():
+    """fp32, two and three pages of up to six, with the gap between chosen and other pages held to what rounding can do.
+
+    A score is a sum of whole numbers.  The device's queries and keys are off by about 2^-20 of a head's largest: a
+    query's 64 elements of up to 2^7 turn to the neighbouring number with a probability of some 2^-12 each, a
+    page's bounds (a code's neighbour, e4m3 steps being 2^-4) with less.  One such turn moves a score by 127 at most
+    (the largest element of a query; bounds are at most 112), so three at once, of which there are none in most runs, stay
+    below 381."""
+    import torch
+    from paper_2508_10259_amd.runtime import DeviceContext
+    spec = small_spec("f32", 2, 256, 4, 512)
+    pair = Pair(spec, seed=65)
+    B, cap, A = 2, 384, 2
+    pre = _prefixes(spec, 297, [330, 200])
+    packed, plens = pair.dev.pack_prefixes(pre)
+    ctx = DeviceContext(pair.dev, B, cap, qcache=True)
+    ctx.build(packed, plens)
+    f64 = pair.prefixes_f64(pre)
+    fed, forced = _forced(5, B, A)
+    for n in (3, 2):
+        ctx.select_pages(n)
+        _, z = ctx.step(A, forced=forced)
+        torch.cuda.synchronize()
+        for b in range(B):
+            r, full = Row(pair, f64[b], cap, n), QuantRow(pair.p, cap)
+            full.commit(f64[b])
+            err = r.step(None, fed[b], z[b].cpu().numpy(), "f32")[0]
+            assert r.q.units > 3 * 127
+            # and over all pages the logits are others, by far more than the device is off
+            want, over_all = z[b].cpu().numpy().astype(np.float64), full.step(None, fed[b])
+            assert np.abs(over_all - want).max() > 10 * err.max()
+    ctx.close()
+
+
 def test_rows_away_on_the_host_come_back_as_they_were():
     import torch
     from paper_2508_10259_amd import capi

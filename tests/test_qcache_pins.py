@@ -74,6 +74,28 @@ def test_bounds_of_a_page_that_began_with_nan():
     assert np.array_equal(c.bounds[0, 0, 1], np.floor(np.nanmin(K, 0) / 4))
 
 
+def test_what_dropped_positions_leave_behind():
+    """A page whose open end is written again and again by positions that are dropped: committed codes are off by less than
+    a subnormal step (2^-9) of the scale that was reached, for all growths together, and the bounds still hold."""
+    rng = np.random.default_rng(9)
+    kept, used = _empty(), _empty()
+    for first in range(0, 60, 3):
+        x = rng.normal(size=(3, 1, 8)) * np.exp2(rng.integers(-12, 1))
+        Q.append(kept, 0, first, x, x)
+        Q.append(used, 0, first, x, x)
+        scratch = rng.normal(size=(4, 1, 8)) * 2.0 ** (first / 5)  # larger every time
+        Q.append(used, 0, first + 3, scratch, scratch)
+    e = int(used.ke[0, 0])
+    assert e >= kept.ke[0, 0] + 8 and e == used.ve[0, 0]
+    for a, b in ((kept.k, used.k), (kept.v.transpose(0, 1, 2, 4, 3).reshape(kept.k.shape), used.v.transpose(0, 1, 2, 4, 3).reshape(kept.k.shape))):
+        a, b = (Q.VALUES[x[0, 0, :60]] * 2.0 ** s for x, s in ((a, int(kept.ke[0, 0])), (b, e)))
+        # (a growth by g >= 1 exponents rounds to half a step of the new scale: 1/2 + 1/4 + ... of the last one's step, and
+        # once where the token itself was rounded at either scale, by half a step or 2^-4 of it)
+        assert np.all(np.abs(a - b) <= 2.0 ** (e - 9) + 2.0 ** -3 * np.abs(a))
+    K = Q.VALUES[used.k[0, 0, :60]]
+    assert np.all(K <= 4 * used.bounds[0, 0, 0]) and np.all(K >= 4 * used.bounds[0, 0, 1])
+
+
 def test_nan_reaches_those_who_see_it_only():
     c = _empty()
     x = np.random.default_rng(4).normal(size=(10, 1, 8))
