@@ -707,7 +707,8 @@ __global__ __launch_bounds__(256, QT == 1 ? (PAIR ? 3 : 4) : 2) void k_qcache_at
   at.settle();
   at.scales();
   // (the first positions are on their way)
-  // queries: scaled by a power of two so that a column's largest element is in [2^10, 2^11)
+  // queries: scaled by a power of two so that a column's largest element is in [2^10, 2^11).  An infinite one makes every
+  // score infinite or NaN, so every output NaN; said at once, since a score of -infinity stands for a masked one here.
   half8 qh[QT][NS], ql[PAIR ? QT : 1][NS];
   float cq[QT];
   int vis[QT], tokc[QT], headc[QT];
@@ -754,7 +755,7 @@ __global__ __launch_bounds__(256, QT == 1 ? (PAIR ? 3 : 4) : 2) void k_qcache_at
     for (int k = 0; k < NS; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float y = ldexpf(x[k][e], 11 - ex);
+        const float y = m < INFINITY ? ldexpf(x[k][e], 11 - ex) : NAN;
         qh[t][k][e] = (f16)y;
         if (PAIR) ql[t][k][e] = (f16)(y - (float)qh[t][k][e]);
       }
@@ -1058,7 +1059,7 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
     for (int k = 0; k < NS; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float z = ldexpf(y[k][e], 11 - ex);
+        const float z = top < INFINITY ? ldexpf(y[k][e], 11 - ex) : NAN;
         qh[k][e] = (f16)z;
         if (PAIR) ql[k][e] = (f16)(z - (float)qh[k][e]);
       }

@@ -416,6 +416,32 @@ def test_nan_and_infinities_reach_only_those_who_see_them():
     b.attend((90,), 4, "f32")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("new", [1, 50])
+def test_queries_with_infinities_and_nan(dtype, new):
+    """A query element of either infinity against keys of either sign, and a NaN: NaN where the query sees anything, zeros
+    where it sees nothing, and no other query touched."""
+    b = Both(2, 2, 2, 64, seed=14)
+
+    def one_sign(t, t64, value=False):
+        if not value:
+            t.abs_().add_(1.0)
+            t[:, 1].neg_()
+            t64[:] = t.double().cpu().numpy()
+    b.append((90, 100), "f16", edit=one_sign)
+    if new > 1:
+        b.lens = [30, 100]  # row 0's first 20 new tokens see nothing
+    G = 3
+    q, q64 = b.tokens((new, new), 2 * G, dtype)
+    for tok, head, x in ((0, 0, math.inf), (0, 4, -math.inf), (new - 1, 1, -math.inf), (new - 1, 3, math.inf), (new, 2, math.nan),
+                         (2 * new - 1, 5, math.inf), (2 * new - 1, 0, -math.inf)):
+        q[tok, head, 7], q64[tok, head, 7] = x, x
+    off, lens = b.where((new, new))
+    got = b.dev.attend(q, off, lens, max_new=new, max_len=100)
+    b.compare(got.double().cpu().numpy(), None, q64, (new, new), G, dtype, 0, 1 / 8)
+    assert int(got.isnan().all(-1).sum()) == (5 if new > 1 else 7)
+
+
 # --- selection ------------------------------------------------------------------------------------
 
 
