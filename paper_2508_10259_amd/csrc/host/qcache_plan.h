@@ -47,9 +47,13 @@ inline QAttendPlan qcache_attend_plan(int n_seg, int n_heads, int n_kv, int dh, 
   const size_t one = (size_t)n_tok * n_heads * (dh + 4);
   const int64_t fit = (int64_t)std::min<size_t>(room / one, 512);
   int64_t s = 1;
-  p.even = p.keys && !n_select && blocks < 768 && steps > QCACHE_LEAST_STEPS;
+  p.even = p.keys && !n_select && blocks < 512 && steps > QCACHE_LEAST_STEPS;
   if (p.even) {
-    // 512 equal pieces, two for each CU; from 256 pairs on 1,536, which the CUs take as they get free
+    // 512 equal pieces, two for each CU; from 256 pairs on 1,536, which the CUs take as they get free.  Rows of 8,000 to
+    // 32,000 positions, 32 heads of 128, bf16, against splits that are dealt alike: 4 rows 126 us (129), 10 rows 298
+    // (325), 12 rows 353 (373); of 1,200 to 2,400: 4 rows 22.2 (20.7), 10 rows 39.6 (38.9), 12 rows 46.5 (42.9).  From 512
+    // pairs on pieces lose at every length: 16 rows 487 (471) and 57.2 (46.4), 23 rows 680 (672) and 74.1 (65.1).  768 and
+    // 1,024 pieces for 4 rows of 70,000 to 131,000 positions, 8 x 4 heads: 162 and 168 us (157 with 512).
     const int64_t pieces = (blocks <= 256 ? 512 : 1536) - blocks;
     s = std::min(pieces / ((int64_t)n_kv * p.tiles), fit);
     p.even = s > n_seg;

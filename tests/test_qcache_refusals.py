@@ -147,6 +147,13 @@ def test_workspace_grows_with_splits_and_lists(lib):
     assert one == 1 < long and listed == 2 * 8 * 4
 
 
+def test_rows_are_cut_into_pieces_below_512_pairs_only(lib):
+    """15 rows of 32 heads leave CUs idle at the ends of ragged rows, 16 fill the GPU by themselves."""
+    sizes = [lib.ams_qcache_workspace_bytes(C.byref(_cache(rows=r, n_kv_heads=32, head_dim=128, pages_per_row=512)), 32, r, 1,
+                                            32000, 0) for r in (15, 16, 20, 23, 24)]
+    assert sizes[0] > 1 and sizes[1:] == [1] * 4
+
+
 def test_python_checks():
     import torch
     from paper_2508_10259_amd.qcache import QuantCache
