@@ -235,8 +235,11 @@ typedef struct {
  * Values saturate at +-65504.  A token whose key or value of a head holds a NaN
  * gets a NaN key there (every query of that head that sees the token reads NaN;
  * none that does not) and zeros for its NaN values.  Tokens at negative
- * positions are not stored.  A page that a call writes is the page of one block of
- * one row (two blocks of a call in one page leave its contents undefined).
+ * positions are not stored.  Positions that a later call writes again, from a smaller
+ * kv_len on, are replaced; what they raised, the page's scale and bounds, stays until
+ * its first position is written.  A page that a call writes is the page of one block of
+ * one row (two blocks of a call in one page leave its contents undefined).  A call
+ * takes at most 2^22 pages and heads: rows * n_kv_heads * ((max_new + 62) / 64 + 1).
  * Errors: AMS_EINVAL, AMS_ENODEV, AMS_EHIP. */
 ams_status ams_qcache_append(const ams_qcache* cache, const int32_t* tok_off, const int32_t* kv_len, int32_t n_tok,
                              int32_t max_new, const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t dtype,

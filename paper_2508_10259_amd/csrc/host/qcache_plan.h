@@ -33,6 +33,9 @@ inline QAttendPlan qcache_attend_plan(int n_seg, int n_heads, int n_kv, int dh, 
                                       int n_select, size_t room = SIZE_MAX) {
   QAttendPlan p{};
   const int64_t G = n_heads / n_kv, cols = n_select ? G : max_new * G;
+  // Up to 32 columns the waves of a workgroup share them, above that each has its own.  64 rows of 216 to 700 positions, 32
+  // heads, 33 new tokens: 104 us, 119 if shared; 48 tokens 105 (119).  Few pairs with 33 to 64 columns would be better off
+  // shared, whose rows can be cut: 4 rows of 8,000 to 16,384, 8 x 4 heads, 9 tokens 48.4 us (39.4), 16 tokens 51.2 (41.2).
   p.keys = n_select > 0 || cols <= 32;
   p.qt = p.keys && (cols <= 16 || n_select) ? 1 : 2;
   const int width = p.keys ? 16 * p.qt : 64 * p.qt;

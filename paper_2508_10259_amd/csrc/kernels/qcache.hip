@@ -425,7 +425,10 @@ __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
 // A wave keeps its columns' running maximum and sum in the lanes that hold them and walks 32-position steps.  With few
 // columns (k_qcache_attend: QT tiles of 16) the four waves share them and deal the steps among themselves, so the cache
 // streams once; with many (k_qcache_attend_wide) each wave has its own and all walk the same steps, whose K/V come from
-// the L1 for three waves of four.  PAIR (fp32 queries): queries and probabilities as fp16 pairs, about 22 bits.
+// the L1 for three waves of four.  PAIR (fp32 queries): queries and probabilities as fp16 pairs, about 22 bits.  fp16 and
+// bf16 queries enter as they are, and their probabilities are rounded to fp16: fp16 outputs are off by 2.3e-4 to 2.9e-4 of
+// their norm (2.0e-4 by their own rounding), bf16 ones by 1.7e-3 with or without.  Pairs would cost a build half as much
+// again (eight prefixes of 2,048 tokens, 8 x 4 heads: 374 us, 564 with them) and a decode 1 to 3% (64 rows: 52.0, 53.4).
 // Measured: few columns are bound by memory (4 rows of 70,000 to 131,000 positions, 8 x 4 heads of 128: 152 us for 0.82
 // GB, 5.4 TB/s; 64 rows of 200 to 768 positions, 32 heads: 51 us for 0.25 GB), many by the vector unit and the products
 // of the same waves taking turns (eight prefixes of 1,500 to 2,048 tokens, 8 x 4 heads: 291 us, 0.72 PFLOP/s).
