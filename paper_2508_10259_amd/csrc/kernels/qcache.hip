@@ -1680,9 +1680,10 @@ template <int D, int NT>
 static hipError_t select_launch(const SelectArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)a.sg.n_seg * a.c.H * ((a.sg.max_new + a.toks - 1) / a.toks);
   const size_t lds = (size_t)a.toks * a.c.ppr * 4;
-  if (lds > 28 * 1024) {  // above 64 KB with the kernel's own
+  // Above 64 KB with the kernel's own.  The limit is the widest table's in every call, so that none lowers another thread's.
+  if (lds > 28 * 1024) {
     hipError_t e = hipFuncSetAttribute((const void*)k_qcache_select<D, NT>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)lds);
+                                       16384 * 4);
     if (e != hipSuccess) return e;
   }
   k_qcache_select<D, NT><<<grid, NT, lds, s>>>(a);

@@ -438,7 +438,8 @@ def test_queries_with_infinities_and_nan(dtype, new):
         q[tok, head, 7], q64[tok, head, 7] = x, x
     off, lens = b.where((new, new))
     got = b.dev.attend(q, off, lens, max_new=new, max_len=100)
-    b.compare(got.double().cpu().numpy(), None, q64, (new, new), G, dtype, 0, 1 / 8)
+    with np.errstate(over="ignore", invalid="ignore"):  # (the tolerance beside an infinity)
+        b.compare(got.double().cpu().numpy(), None, q64, (new, new), G, dtype, 0, 1 / 8)
     assert int(got.isnan().all(-1).sum()) == (5 if new > 1 else 7)
 
 
@@ -672,6 +673,76 @@ def test_two_streams_and_repeated_calls_give_the_same_bits():
         assert torch.equal(a, outs[0])
     for a in outs[3::2]:
         assert torch.equal(a, outs[1])
+
+
+def _wide(ppr, seed, G=2):
+    """A row of ppr pages of which forty lie in the pool, a query over it, and the call that selects eight of them."""
+    import torch
+    from paper_2508_10259_amd.qcache import QuantCache
+    b = Both(1, 40, 1, 64, seed=seed)
+    b.append((40 * 64,), "f16")
+    table = np.full((1, ppr), -1, np.int32)
+    at = np.sort(b.rng.choice(ppr - 1, 39, replace=False))
+    table[0, at], table[0, ppr - 1] = b.ref.table[0, :39], b.ref.table[0, 39]
+    b.ref.table, b.lens = table, [ppr * 64]
+    d = b.dev
+    b.dev = QuantCache(d.k, d.v, d.k_scale, d.v_scale, d.k_bounds, torch.from_numpy(table).cuda())
+    q, q64 = b.tokens((1,), G, "f16")
+    off, lens = b.where((1,))
+    return b, q, q64, lambda: b.dev.attend_selected(q, off, lens, 8, max_new=1)
+
+
+def test_two_threads_select_over_tables_of_different_widths():
+    """Calls at once on two streams, whose selections take different amounts of LDS: each gives what it gives alone."""
+    import threading
+    import torch
+    calls = [_wide(ppr, 53 + ppr) for ppr in (16384, 9000)]
+    alone = []
+    for b, q, q64, call in calls:
+        out, sel = call()
+        torch.cuda.synchronize()
+        b.compare(out.double().cpu().numpy(), sel.cpu().numpy(), q64, (1,), 2, "f16", 8, 1 / 8)
+        alone.append((out, sel))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(n):
+        try:
+            torch.cuda.set_device(0)
+            with torch.cuda.stream(torch.cuda.Stream()):
+                got = [calls[n][3]() for _ in range(300)]
+                torch.cuda.current_stream().synchronize()
+            wrong.extend((n, i) for i, g in enumerate(got) for x, y in zip(g, alone[n]) if not torch.equal(x, y))
+        except Exception as e:  # noqa: BLE001 (handed to the test's thread)
+            wrong.append((n, e))
+    threads = [threading.Thread(target=work, args=(n,)) for n in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong[:3]
+
+
+def test_a_selection_over_the_widest_table_in_a_graph():
+    import torch
+    b, q, q64, call = _wide(16384, 54)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, sel = call()
+    for r in range(4):
+        x = torch.from_numpy(b.rng.normal(size=tuple(q.shape))).half()
+        q.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        b.compare(out.double().cpu().numpy(), sel.cpu().numpy(), x.double().numpy(), (1,), 2, "f16", 8, 1 / 8)
+        narrow = _wide(200, 60 + r)[3]()  # eager work between the replays
+        torch.cuda.synchronize()
+        assert int(narrow[1].min()) >= 0
 
 
 def test_results_do_not_depend_on_other_rows():
