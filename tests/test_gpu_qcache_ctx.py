@@ -225,6 +225,79 @@ def test_shared_prefix_pages():
     ctx.close()
 
 
+@pytest.mark.parametrize("dtype,n_select", [("f32", 0), ("bf16", 0), ("f32", 40)])
+def test_a_decode_over_rows_in_pieces(dtype, n_select):
+    """Rows long enough to be cut, and selections too: the pieces' sums are joined into the decode's output and its
+    rounding errors.  40 of row 0's 41 pages are chosen, with a gap above two turns of a whole number."""
+    import torch
+    from paper_2508_10259_amd.runtime import DeviceContext
+    spec = small_spec(dtype, 1, 128, 2, 256)
+    pair = Pair(spec, seed=81)
+    lens, cap, A, seed = [2600, 30, 1150], 4096, 4, 217
+    pre = _prefixes(spec, seed, lens)
+    packed, plens = pair.dev.pack_prefixes(pre)
+    ctx = DeviceContext(pair.dev, 3, cap, qcache=True)
+    ctx.build(packed, plens)
+    ctx.select_pages(n_select)
+    f64 = pair.prefixes_f64(pre)
+    for s in range(2):
+        fed, forced = _forced(s, 3, A)
+        news = [W.make_observation(spec, seed, 20 + s, b, n) for b, n in enumerate((5, 1, 2))]
+        nt, nl = gpu_new_tokens(spec, news)
+        _, z = ctx.step(A, nt, nl, forced=forced)
+        torch.cuda.synchronize()
+        if s == 0:
+            refs = [Row(pair, f64[b], cap, n_select) for b in range(3)]
+        for b in range(3):
+            refs[b].step(news[b], fed[b], z[b].cpu().numpy(), dtype)
+    assert refs[0].q.units > 2 * 127
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype,B,share", [("bf16", 3, False), ("f32", 70, False), ("bf16", 70, True)])
+def test_replayed_steps_give_what_new_ones_give(dtype, B, share):
+    """Steps into the same buffers (one captured graph, replayed) and into new ones, over page ends, changed selections and rows
+    that leave for the host: the same bits."""
+    import torch
+    from paper_2508_10259_amd.runtime import DeviceContext
+    spec = small_spec(dtype, 2, 256, 4, 512)
+    pair = Pair(spec, seed=91)
+    lens = [int(x) for x in np.random.default_rng(B).integers(100, 300, size=B)]
+    scene = W.random_gaussian((90, spec.d_model), 91, 500, dtype=dtype)
+    pre = [W.Prefix(np.concatenate([scene, W.make_observation(spec, 91, 0, b, n - 90)]), np.zeros(0, np.int32))
+           for b, n in enumerate(lens)]
+    packed, plens = pair.dev.pack_prefixes(pre)
+    kept, fresh = (DeviceContext(pair.dev, B, 512, share_prefix=share, qcache=True) for _ in range(2))
+    for c in (kept, fresh):
+        c.build(packed, plens)
+    A = 3
+    tok = torch.empty(B, A, dtype=torch.int32, device="cuda")
+    logits = torch.empty(B, A, spec.n_bins, device="cuda")
+    forced = torch.empty(B, A, dtype=torch.int32, device="cuda")
+    now = list(lens)
+    for s in range(8):
+        forced.copy_(_forced(s, B, A)[1])
+        n_new = [(7 * b + 5 * s) % 23 for b in range(B)]
+        news = [W.make_observation(spec, 91, 20 + s, b, n) if n else None for b, n in enumerate(n_new)]
+        nt, nl = gpu_new_tokens(spec, news)
+        now = [x + n for x, n in zip(now, n_new)]
+        for c in (kept, fresh):
+            c.select_pages((0, 2, 0, 4, 3, 2, 0, 9)[s])
+        if s == 5:
+            row = B // 2
+            for c in (kept, fresh):
+                buf = torch.empty(c.row_host_bytes(now[row] - n_new[row]), dtype=torch.uint8).pin_memory()
+                c.offload_rows([row], [buf])
+                c.reload_rows([row], [buf])
+        kept.step(A, nt, nl, tokens=tok, logits=logits, forced=forced)
+        t, z = fresh.step(A, nt, nl, forced=forced.clone())
+        torch.cuda.synchronize()
+        assert torch.equal(z, logits) and torch.equal(t, tok), s
+        assert bool(torch.isfinite(z).all())
+    for c in (kept, fresh):
+        c.close()
+
+
 def test_flow_over_8_bit_contexts():
     import torch
     from paper_2508_10259_amd.runtime import DeviceContext, DeviceFlowHead
