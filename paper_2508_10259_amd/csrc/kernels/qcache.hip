@@ -431,7 +431,7 @@ __global__ __launch_bounds__(NT) void k_qcache_append(AppendArgs a) {
 // again (eight prefixes of 2,048 tokens, 8 x 4 heads: 374 us, 564 with them) and a decode 1 to 3% (64 rows: 52.0, 53.4).
 // Measured: few columns are bound by memory (4 rows of 70,000 to 131,000 positions, 8 x 4 heads of 128: 152 us for 0.82
 // GB, 5.4 TB/s; 64 rows of 200 to 768 positions, 32 heads: 51 us for 0.25 GB), many by the vector unit and the products
-// of the same waves taking turns (eight prefixes of 1,500 to 2,048 tokens, 8 x 4 heads: 291 us, 0.72 PFLOP/s).
+// of the same waves taking turns (eight prefixes of 1,500 to 2,048 tokens, 8 x 4 heads: 293 us, 0.71 PFLOP/s).
 
 struct AttendArgs {
   QCache c;
