@@ -28,9 +28,10 @@ struct QAttendPlan {
 };
 
 // A call of n_seg segments of at most max_new tokens, n_tok in all, over about max_len positions (n_select > 0:
-// over that many pages of 64 for each token); room: floats there are for partial sums.
+// over that many pages of 64 for each token); room: floats there are for partial sums; even_below: pairs of a segment and
+// a KV head (times its tiles) below which rows are cut into equal pieces.
 inline QAttendPlan qcache_attend_plan(int n_seg, int n_heads, int n_kv, int dh, int n_tok, int max_new, int max_len,
-                                      int n_select, size_t room = SIZE_MAX) {
+                                      int n_select, size_t room = SIZE_MAX, int even_below = 512) {
   QAttendPlan p{};
   const int64_t G = n_heads / n_kv, cols = n_select ? G : max_new * G;
   // Up to 32 columns the waves of a workgroup share them, above that each has its own.  64 rows of 216 to 700 positions, 32
@@ -50,7 +51,7 @@ inline QAttendPlan qcache_attend_plan(int n_seg, int n_heads, int n_kv, int dh, 
   const size_t one = (size_t)n_tok * n_heads * (dh + 4);
   const int64_t fit = (int64_t)std::min<size_t>(room / one, 512);
   int64_t s = 1;
-  p.even = p.keys && !n_select && blocks < 512 && steps > QCACHE_LEAST_STEPS;
+  p.even = p.keys && !n_select && blocks < even_below && steps > QCACHE_LEAST_STEPS;
   if (p.even) {
     // 512 equal pieces, two for each CU; from 256 pairs on 1,536, which the CUs take as they get free.  Rows of 8,000 to
     // 32,000 positions, 32 heads of 128, bf16, against splits that are dealt alike: 4 rows 126 us (129), 10 rows 298

@@ -265,8 +265,10 @@ inline CtxLayout ctx_layout(const Cfg& c, int batch, int capacity, int pass_toke
   if (qcache) {  // (each layer's arrays 256-byte aligned)
     x.scale_layer = align256((size_t)x.n_pages * c.n_heads * 4);
     x.bound_layer = align256((size_t)x.n_pages * 2 * d);
+    // Room for the pieces of a decode pass; with 512 to 767 pairs, which decode in one piece, as much as 1,536 pieces take,
+    // for the splits of passes of a few of the rows.
     x.qc_part_floats =
-        qcache_attend_plan(batch, c.n_heads, c.n_heads, c.head_dim, batch, 1, capacity, 0).part_floats;
+        qcache_attend_plan(batch, c.n_heads, c.n_heads, c.head_dim, batch, 1, capacity, 0, SIZE_MAX, 768).part_floats;
   }
   x.qc_scale = o; o = align256(o + 2 * L * x.scale_layer);
   x.qc_bound = o; o = align256(o + L * x.bound_layer);

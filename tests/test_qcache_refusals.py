@@ -154,6 +154,17 @@ def test_rows_are_cut_into_pieces_below_512_pairs_only(lib):
     assert sizes[0] > 1 and sizes[1:] == [1] * 4
 
 
+def test_contexts_keep_room_for_the_splits_of_a_few_rows(lib):
+    """16 rows of 32 heads decode in one piece each, and an extension of some of them is cut: 32 pieces a row."""
+    from paper_2508_10259_amd.capi import AMS_CTX_QCACHE, ModelCfg
+    cfg = C.byref(ModelCfg(1, 2048, 32, 64, 1024, 256, 256, 1e-5, 1e4, 1))
+    size = [lib.ams_ctx_workspace_bytes_paged(cfg, b, 1088, 8192, 0, AMS_CTX_QCACHE) for b in (15, 16, 23, 24)]
+    parts = [n * 32 * 68 * 4 * p for n, p in ((15, 33), (16, 32), (23, 25), (24, 0))]  # (1,536 - pairs) / heads pieces
+    row = 17 * (2 * 64 * 2048 + 32 * 8 + 2 * 2048)  # K/V, scales and bounds of a row's pages
+    for n, a, b, pa, pb in zip((1, 7, 1), size, size[1:], parts, parts[1:]):
+        assert 0 <= b - a - (pb - pa) - n * row < 0.15 * n * row
+
+
 def test_python_checks():
     import torch
     from paper_2508_10259_amd.qcache import QuantCache
