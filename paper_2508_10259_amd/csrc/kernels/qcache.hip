@@ -758,10 +758,11 @@ __global__ __launch_bounds__(256, QT == 1 ? (PAIR ? 3 : 4) : 2) void k_qcache_at
     for (int k = 0; k < NS; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float y = m < INFINITY ? ldexpf(x[k][e], 11 - ex) : NAN;
+        const float y = ldexpf(x[k][e], 11 - ex);
         qh[t][k][e] = (f16)y;
         if (PAIR) ql[t][k][e] = (f16)(y - (float)qh[t][k][e]);
       }
+    if (m == INFINITY) qh[t][0][0] = (f16)NAN;
   }
   // One step; EDGE: some of its positions are masked for a column, or lie behind the row's last one.  MORE: the next
   // one's loads go out as its registers get free, without a condition, so that each wait is for what it needs alone.
@@ -1062,10 +1063,11 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
     for (int k = 0; k < NS; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float z = top < INFINITY ? ldexpf(y[k][e], 11 - ex) : NAN;
+        const float z = ldexpf(y[k][e], 11 - ex);
         qh[k][e] = (f16)z;
         if (PAIR) ql[k][e] = (f16)(z - (float)qh[k][e]);
       }
+    if (top == INFINITY) qh[0][0] = (f16)NAN;
   }
 
   f32x16 o[NJ];
@@ -1131,15 +1133,13 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attend_wide(AttendArgs a) {
     // prefixes of 1,500 to 2,048 tokens, 8 x 4 heads of 128)
     if (far) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = mul_rounded(sc[r], cs) - base;
-    } else {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = fmaf(sc[r], cs, -base);
+      for (int r = 0; r < 16; ++r) sc[r] = mul_rounded(sc[r], cs);
     }
+    const float slope = far ? 1.f : cs;
     half8 ph8[2], pl8[PAIR ? 2 : 1];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const float p = __builtin_amdgcn_exp2f(sc[r]);
+      const float p = __builtin_amdgcn_exp2f(fmaf(sc[r], slope, -base));
       ph8[r / 8][r % 8] = (f16)p;
       if (PAIR) {
         pl8[r / 8][r % 8] = (f16)(p - (float)ph8[r / 8][r % 8]);
