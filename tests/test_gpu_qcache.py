@@ -216,6 +216,19 @@ def test_append_of_many_tokens_to_pages_whose_scale_grows(D, n):
     b.check()
 
 
+@pytest.mark.parametrize("D,dtype", [(64, "f16"), (128, "f32"), (128, "bf16")])
+def test_positions_that_are_written_again(D, dtype):
+    """Rows that drop their last positions and go on from there, inside a page, at its end and several pages back."""
+    b = Both(4, 5, 2, D, seed=56)
+    b.append((200, 64, 130, 90), dtype)
+    for back, counts, std in (((3, 1, 2, 26), (5, 2, 2, 30), 4.0), ((73, 65, 66, 94), (1, 70, 3, 5), 0.1), ((1, 60, 0, 4), (64, 3, 9, 40), 50.0)):
+        b.lens = [n - x for n, x in zip(b.lens, back)]
+        b.append(counts, dtype, std)
+        b.check()
+        for new, n_select in (((1, 1, 1, 1), 0), ((1, 2, 2, 5), 2)):
+            b.attend(new, 2, dtype, n_select=n_select)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("counts", [(1, 1), (2, 30), (40, 1), (20, 44)])
 def test_bounds_of_pages_that_began_with_nan(D, counts):
